@@ -384,6 +384,83 @@ atp_status atp_norm_factored(const void* P, const void* C, const float* gain, fl
                              size_t workspace_bytes, atp_dtype t, void* hip_stream);
 
 /* --------------------------------------------------------------------------
+ * Serving: prompts packed one behind the other, a paged cache of keys and values, attention over it.
+ *
+ * Tokens of several sequences lie one behind the other in [tokens, heads, d_h] tensors; `offsets` [n_seq + 1] (device int32) says where
+ * each sequence starts: tokens offsets[s] … offsets[s+1] − 1 belong to sequence s (none when both are equal).  Rows outside every sequence
+ * are neither read nor written.  A token's row of heads·d_h elements is contiguous, rows are a stride (ldq, ldk, ldv, ldo, in elements)
+ * apart, so Q, K and V may be column blocks of one packed projection.  Every stride is a multiple of 16 bytes and at least the row.
+ * `heads` is a multiple of `kv_heads`: query head h reads key head h / (heads / kv_heads).  d_h is a multiple of 8 up to 256.
+ * Offsets are read on the device only: they may change between replays of a captured graph, as long as `tokens` and `n_seq` stay.
+ * Values outside 0 … tokens are taken to the nearest bound, a sequence that ends before it starts is empty, and the sequences of offsets
+ * that decrease are computed in an undefined way, within the tensors.
+ * -------------------------------------------------------------------------- */
+
+/* Storage of a cache: the type of the call, or 8-bit floats (1 sign, 4 exponent, 3 mantissa bits; largest value 448) with a power of two
+ * for every row of d_h elements: element = value · 2^(scale − 127).  Writing takes the smallest power of two (from 2^−127 on) that brings the
+ * finite elements of the row into ±448 and rounds to nearest even; elements that are not finite become NaN.  Both factors being exact, what
+ * a code stands for is exact in either storage type. */
+typedef enum { ATP_CACHE_SAME = 0, ATP_CACHE_E4M3 = 1 } atp_cache_type;
+
+/* Pages of page_size positions (a power of two up to 65536); page p of a cache holds positions of one sequence, which one is said by the
+ * table of each call.  All pointers device, 16-byte aligned, read or written where they point: there is nothing to set up or destroy. */
+typedef struct {
+    void* K;               /* [n_pages, kv_heads, page_size, d_h]  type t or 8-bit codes */
+    void* V;               /* same */
+    uint8_t* K_scale;      /* [n_pages, kv_heads, page_size]  biased exponents; ATP_CACHE_E4M3 only, else NULL */
+    uint8_t* V_scale;
+    int64_t n_pages;
+    int32_t page_size, kv_heads, d_h;
+    atp_cache_type type;
+} atp_cache;
+
+/* Sequences of a call.  The new tokens of sequence s are its last n_s = offsets[s+1] − offsets[s] positions: token i of them has position
+ * length[s] − n_s + i, which lies in page table[s·max_pages + position / page_size].  A position below 0, at or above
+ * max_pages·page_size, or whose page number is not in 0 … n_pages − 1 (−1 for "none") has no place: writing skips it, reading gives zeros
+ * and attention sees no key there. */
+typedef struct {
+    const int32_t* table;     /* [n_seq, max_pages] device */
+    const int32_t* length;    /* [n_seq] device; positions of the sequence, the new tokens included */
+    const int32_t* offsets;   /* [n_seq + 1] device */
+    int64_t n_seq, max_pages;
+    int64_t tokens;           /* rows of the packed tensors; 0: the call does nothing */
+} atp_batch;
+
+/* Rows of the new tokens into their places in the cache.  K, V [tokens, kv_heads, d_h] (type t).  Two tokens with one place (a page that
+ * two sequences share and both write) leave one of their rows there, whole or mixed.
+ * Errors: ATP_ERR_INVALID_ARG (null, misaligned, bad size, stride or enum), ATP_ERR_DEVICE. */
+atp_status atp_cache_write(const atp_cache* cache, const atp_batch* batch, const void* K, const void* V, int64_t ldk, int64_t ldv,
+                           atp_dtype t, void* hip_stream);
+
+/* The inverse: rows of the last n_s positions of every sequence, as type t.  Arguments and errors as atp_cache_write. */
+atp_status atp_cache_read(const atp_cache* cache, const atp_batch* batch, void* K, void* V, int64_t ldk, int64_t ldv, atp_dtype t,
+                          void* hip_stream);
+
+/* Attention of every sequence over its own tokens:
+ *     O[i, h] = Σ_j softmax_j(scale · <Q[i, h], K[j, h / (heads/kv_heads)]>) · V[j, h / (heads/kv_heads)],
+ * j over the tokens of the sequence, with `causal` (not 0) those up to i.  scale <= 0: 1/sqrt(d_h).  Values of keys that a query does not
+ * see never reach it, also when they are not finite.  A query all of whose scores are −inf gives zeros.
+ * Workspace: 0 bytes for some shapes; depends on sizes only.
+ * Errors: ATP_ERR_INVALID_ARG, ATP_ERR_UNSUPPORTED (d_h above 256 or no multiple of 8; tokens·heads >= 2^31), ATP_ERR_WORKSPACE,
+ * ATP_ERR_DEVICE. */
+size_t atp_attention_packed_workspace(int64_t n_seq, int64_t tokens, int heads, int kv_heads, int d_h, atp_dtype t);
+
+atp_status atp_attention_packed(const void* Q, const void* K, const void* V, void* O, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo,
+                                const int32_t* offsets, int64_t n_seq, int64_t tokens, int heads, int kv_heads, int d_h, int causal,
+                                float scale, void* workspace, size_t workspace_bytes, atp_dtype t, void* hip_stream);
+
+/* Attention of the new tokens over the pages of their sequence (which hold the new tokens' own keys already): j over the positions below
+ * length[s], with `causal` those up to the token's own.  A query that sees no key gives zeros.  Without `causal` and with r_s principal keys
+ * in the pages of sequence s it is atp_attention with a rank of its own for every sequence.
+ * max_new: largest n_s that the caller expects, 0 if unknown.  It only chooses how the work is dealt; larger n_s are computed as well.
+ * Errors as atp_attention_packed; ATP_ERR_UNSUPPORTED also for max_pages·page_size > 2^30. */
+size_t atp_attention_paged_workspace(const atp_cache* cache, const atp_batch* batch, int heads, int64_t max_new, atp_dtype t);
+
+atp_status atp_attention_paged(const void* Q, const atp_cache* cache, const atp_batch* batch, void* O, int64_t ldq, int64_t ldo, int heads,
+                               int causal, float scale, int64_t max_new, void* workspace, size_t workspace_bytes, atp_dtype t,
+                               void* hip_stream);
+
+/* --------------------------------------------------------------------------
  * Kernel timing with HIP events (diagnostic; used by the benchmark to measure
  * per-kernel durations live, on the stream the kernels are launched on).
  * While a class bit is enabled every launch of that class is bracketed by two

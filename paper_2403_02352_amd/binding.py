@@ -24,6 +24,16 @@ class AtpError(RuntimeError):
         super().__init__(f"{where}: {lib.atp_status_string(status).decode()} (status {status})")
 
 
+class _Cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_scale", C.c_void_p), ("V_scale", C.c_void_p), ("n_pages", C.c_int64),
+                ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("d_h", C.c_int32), ("type", C.c_int)]
+
+
+class _Batch(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("length", C.c_void_p), ("offsets", C.c_void_p), ("n_seq", C.c_int64), ("max_pages", C.c_int64),
+                ("tokens", C.c_int64)]
+
+
 def _load() -> C.CDLL:
     p = lib_path()
     if not os.path.exists(p):
@@ -86,6 +96,19 @@ def _load() -> C.CDLL:
     L.atp_attention_linearised_workspace.argtypes = [i64, i64, i64, i64, i32, i32]
     L.atp_attention_linearised.restype = i32
     L.atp_attention_linearised.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, C.c_float, i32, vp, sz, i32, vp]
+    pc, pb = C.POINTER(_Cache), C.POINTER(_Batch)
+    L.atp_cache_write.restype = i32
+    L.atp_cache_write.argtypes = [pc, pb, vp, vp, i64, i64, i32, vp]
+    L.atp_cache_read.restype = i32
+    L.atp_cache_read.argtypes = [pc, pb, vp, vp, i64, i64, i32, vp]
+    L.atp_attention_packed_workspace.restype = sz
+    L.atp_attention_packed_workspace.argtypes = [i64, i64, i32, i32, i32, i32]
+    L.atp_attention_packed.restype = i32
+    L.atp_attention_packed.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, vp, i64, i64, i32, i32, i32, i32, C.c_float, vp, sz, i32, vp]
+    L.atp_attention_paged_workspace.restype = sz
+    L.atp_attention_paged_workspace.argtypes = [pc, pb, i32, i64, i32]
+    L.atp_attention_paged.restype = i32
+    L.atp_attention_paged.argtypes = [vp, pc, pb, vp, i64, i64, i32, i32, C.c_float, i64, vp, sz, i32, vp]
     L.atp_profile_enable.restype = None
     L.atp_profile_enable.argtypes = [C.c_uint]
     L.atp_profile_reset.restype = None
@@ -421,6 +444,173 @@ def attention_linearised(Q: torch.Tensor, K_r: torch.Tensor, V_r: torch.Tensor, 
                                       float(scale), norm, _ptr(ws), 0 if ws is None else ws.numel(), _dt(Q), _stream())
     if st != 0:
         raise AtpError(st, "atp_attention_linearised")
+    return out
+
+
+ATP_CACHE_SAME, ATP_CACHE_E4M3 = 0, 1
+
+
+class PagedCache:
+    """Pages of keys and values, [n_pages, kv_heads, page_size, d_h] each: in the storage type of the calls, or as torch.float8_e4m3fn
+    codes with a biased exponent (uint8 [n_pages, kv_heads, page_size]) for every row.  The tensors stay the caller's."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: Optional[torch.Tensor] = None, V_scale: Optional[torch.Tensor] = None):
+        _check(K, V, K_scale, V_scale)
+        e4m3 = K.dtype == torch.float8_e4m3fn
+        if K.dim() != 4 or V.shape != K.shape or V.dtype != K.dtype:
+            raise ValueError("K and V must be [n_pages, kv_heads, page_size, d_h] of one type")
+        if not e4m3:
+            _dt(K)
+        for s in (K_scale, V_scale):
+            if (s is not None) != e4m3:
+                raise ValueError("float8_e4m3fn pages have scales, others none")
+            if s is not None and (s.dtype != torch.uint8 or s.shape != K.shape[:3]):
+                raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
+        self.device = _one_device(K, V, K_scale, V_scale)
+        self.K, self.V, self.K_scale, self.V_scale = K, V, K_scale, V_scale
+        self.n_pages, self.kv_heads, self.page_size, self.d_h = K.shape
+        p = lambda t: None if t is None else t.data_ptr()
+        self._c = _Cache(p(K), p(V), p(K_scale), p(V_scale), self.n_pages, self.page_size, self.kv_heads, self.d_h,
+                         ATP_CACHE_E4M3 if e4m3 else ATP_CACHE_SAME)
+
+    @classmethod
+    def empty(cls, n_pages: int, kv_heads: int, page_size: int, d_h: int, dtype: torch.dtype, device="cuda") -> "PagedCache":
+        """A cache of zeros; dtype torch.float8_e4m3fn for 8 bits."""
+        shape = (n_pages, kv_heads, page_size, d_h)
+        if dtype != torch.float8_e4m3fn:
+            return cls(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device))
+        codes = lambda: torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype)
+        scale = lambda: torch.zeros(shape[:3], dtype=torch.uint8, device=device)
+        return cls(codes(), codes(), scale(), scale())
+
+
+def _one_device(*ts) -> torch.device:
+    dev = {t.device for t in ts if t is not None}
+    if len(dev) != 1 or next(iter(dev)).type != "cuda":
+        raise ValueError("tensors must live on one GPU")
+    return dev.pop()
+
+
+def _rows(t: torch.Tensor, name: str, heads: Optional[int] = None, d_h: Optional[int] = None) -> int:
+    """Row stride of a packed [tokens, heads, d_h] tensor, whose rows may be a column block of a wider matrix."""
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (d_h is not None and t.shape[2] != d_h):
+        raise ValueError(f"{name} must be [tokens, heads, d_h]")
+    row = t.shape[1] * t.shape[2]
+    if t.numel() == 0:
+        return row
+    if (t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"the heads of a row of {name} must lie one behind the other")
+    return t.stride(0) if t.shape[0] > 1 else row
+
+
+def _int32(name: str, t: torch.Tensor, dim: int) -> None:
+    if t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous int32 with {dim} dimension(s)")
+
+
+def _batch(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: int) -> _Batch:
+    _int32("table", table, 2)
+    _int32("length", length, 1)
+    _int32("offsets", offsets, 1)
+    n_seq, max_pages = table.shape
+    if length.shape[0] != n_seq or offsets.shape[0] != n_seq + 1:
+        raise ValueError("table [n_seq, max_pages], length [n_seq] and offsets [n_seq + 1] do not match")
+    return _Batch(table.data_ptr(), length.data_ptr(), offsets.data_ptr(), n_seq, max_pages, tokens)
+
+
+def _serving(status: int, where: str) -> None:
+    if status != 0:
+        raise AtpError(status, where)
+
+
+def cache_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor) -> None:
+    """Rows of the new tokens K, V [tokens, kv_heads, d_h] into their pages: token i of the n new ones of sequence s goes to position
+    length[s] - n + i, page table[s, position // page_size].  offsets [n_seq + 1]: where each sequence's tokens start."""
+    dev = _one_device(cache.K, K, V, table, length, offsets)
+    ldk, ldv = _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V", cache.kv_heads, cache.d_h)
+    if V.shape != K.shape or V.dtype != K.dtype or cache._c.type == ATP_CACHE_SAME and K.dtype != cache.K.dtype:
+        raise ValueError("K / V shape or dtype mismatch")
+    b = _batch(cache, table, length, offsets, K.shape[0])
+    with torch.cuda.device(dev):
+        _serving(lib.atp_cache_write(cache._c, b, K.data_ptr(), V.data_ptr(), ldk, ldv, _dt(K), _stream()), "atp_cache_write")
+
+
+def cache_read(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: Optional[int] = None,
+               dtype: Optional[torch.dtype] = None, out=None):
+    """The last offsets[s+1] - offsets[s] positions of every sequence -> (K, V) [tokens, kv_heads, d_h].  `out`: such a pair; rows of it
+    outside every sequence stay.  Without it `tokens` (the rows to make, zeros outside every sequence) is wanted, and for an 8-bit cache
+    `dtype`."""
+    if out is None:
+        if tokens is None or (dtype is None and cache._c.type == ATP_CACHE_E4M3):
+            raise ValueError("without `out`, tokens (and dtype for an 8-bit cache) must be given")
+        dt = cache.K.dtype if dtype is None else dtype
+        out = tuple(torch.zeros((tokens, cache.kv_heads, cache.d_h), dtype=dt, device=cache.device) for _ in range(2))
+    K, V = out
+    dev = _one_device(cache.K, K, V, table, length, offsets)
+    ldk, ldv = _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V", cache.kv_heads, cache.d_h)
+    if V.shape != K.shape or V.dtype != K.dtype or cache._c.type == ATP_CACHE_SAME and K.dtype != cache.K.dtype:
+        raise ValueError("K / V shape or dtype mismatch")
+    b = _batch(cache, table, length, offsets, K.shape[0])
+    with torch.cuda.device(dev):
+        _serving(lib.atp_cache_read(cache._c, b, K.data_ptr(), V.data_ptr(), ldk, ldv, _dt(K), _stream()), "atp_cache_read")
+    return K, V
+
+
+def attention_packed_workspace(n_seq, tokens, heads, kv_heads, d_h, dtype) -> int:
+    return lib.atp_attention_packed_workspace(n_seq, tokens, heads, kv_heads, d_h, _DT[dtype])
+
+
+def attention_packed(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, offsets: torch.Tensor, causal: bool = True, scale: float = 0.0,
+                     workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of packed sequences over their own tokens: Q [tokens, heads, d_h], K, V [tokens, kv_heads, d_h], offsets [n_seq + 1] -> O.
+    Rows outside every sequence keep what `out` held (zeros without it)."""
+    dev = _one_device(Q, K, V, offsets, *(t for t in (workspace, out) if t is not None))
+    _int32("offsets", offsets, 1)
+    ldq, ldk = _rows(Q, "Q"), _rows(K, "K", None, Q.shape[2])
+    ldv = _rows(V, "V", K.shape[1], Q.shape[2])
+    tokens, heads, d_h = Q.shape
+    kv_heads, n_seq = K.shape[1], offsets.shape[0] - 1
+    if K.shape[0] != tokens or V.shape[0] != tokens or K.dtype != Q.dtype or V.dtype != Q.dtype:
+        raise ValueError("K / V shape or dtype mismatch")
+    t = _dt(Q)
+    if out is None:
+        out = torch.zeros((tokens, heads, d_h), dtype=Q.dtype, device=dev)
+    elif out.shape != Q.shape or out.dtype != Q.dtype:
+        raise ValueError("out must have the shape and dtype of Q")
+    ldo = _rows(out, "out")
+    ws = _ws(lib.atp_attention_packed_workspace(n_seq, tokens, heads, kv_heads, d_h, t), Q, workspace)
+    with torch.cuda.device(dev):
+        _serving(lib.atp_attention_packed(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), ldq, ldk, ldv, ldo, offsets.data_ptr(),
+                                          n_seq, tokens, heads, kv_heads, d_h, 1 if causal else 0, float(scale), _ptr(ws),
+                                          0 if ws is None else ws.numel(), t, _stream()), "atp_attention_packed")
+    return out
+
+
+def attention_paged_workspace(cache: PagedCache, n_seq, max_pages, tokens, heads, dtype, max_new: int = 0) -> int:
+    return lib.atp_attention_paged_workspace(cache._c, _Batch(None, None, None, n_seq, max_pages, tokens), heads, max_new, _DT[dtype])
+
+
+def attention_paged(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor,
+                    causal: bool = True, scale: float = 0.0, max_new: int = 0, workspace: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens Q [tokens, heads, d_h] over the pages of their sequence (their own keys are there already).
+    max_new: the largest number of new tokens of a sequence, if known (a hint)."""
+    dev = _one_device(cache.K, Q, table, length, offsets, *(t for t in (workspace, out) if t is not None))
+    ldq = _rows(Q, "Q", None, cache.d_h)
+    tokens, heads, d_h = Q.shape
+    t = _dt(Q)
+    if cache._c.type == ATP_CACHE_SAME and Q.dtype != cache.K.dtype:
+        raise ValueError("Q and the cache differ in dtype")
+    if out is None:
+        out = torch.zeros((tokens, heads, d_h), dtype=Q.dtype, device=dev)
+    elif out.shape != Q.shape or out.dtype != Q.dtype:
+        raise ValueError("out must have the shape and dtype of Q")
+    ldo = _rows(out, "out")
+    b = _batch(cache, table, length, offsets, tokens)
+    ws = _ws(lib.atp_attention_paged_workspace(cache._c, b, heads, max_new, t), Q, workspace)
+    with torch.cuda.device(dev):
+        _serving(lib.atp_attention_paged(Q.data_ptr(), cache._c, b, out.data_ptr(), ldq, ldo, heads, 1 if causal else 0, float(scale), max_new,
+                                         _ptr(ws), 0 if ws is None else ws.numel(), t, _stream()), "atp_attention_paged")
     return out
 
 

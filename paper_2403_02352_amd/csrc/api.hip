@@ -1,10 +1,8 @@
 // C ABI of the ATP library: argument checks, workspace carve-up and the host-side
 // sequencing of kernels.  Nothing here allocates or synchronises.
-#include "../../include/atp.h"
-#include "common.h"
+#include "api_common.h"
 
 #include <algorithm>
-#include <cstring>
 #include <vector>
 
 using namespace atp;
@@ -24,20 +22,21 @@ hipEvent_t prof_event() {
     return e;
 }
 
-struct ProfScope {
-    hipStream_t st; bool on = false; ProfRec rec;
-    ProfScope(hipStream_t s, int cls, double flops, double bytes) : st(s) {
-        if (g_prof_mask & (1u << cls)) {
-            on = true;
-            rec.cls = cls; rec.flops = flops; rec.bytes = bytes;
-            rec.a = prof_event(); rec.b = prof_event();
-            (void)hipEventRecord(rec.a, st);
-        }
-    }
-    ~ProfScope() {
-        if (on) { (void)hipEventRecord(rec.b, st); g_recs.push_back(rec); }
-    }
-};
+}  // namespace
+
+atp::ProfScope::ProfScope(hipStream_t s, int c, double fl, double by) : st(s), cls(c), flops(fl), bytes(by) {
+    if (!(g_prof_mask & (1u << cls))) return;
+    a = prof_event();
+    b = prof_event();
+    (void)hipEventRecord(a, st);
+}
+atp::ProfScope::~ProfScope() {
+    if (!b) return;
+    (void)hipEventRecord(b, st);
+    g_recs.push_back({cls, a, b, flops, bytes});
+}
+
+namespace {
 
 int g_passes_first = 2, g_passes_middle = 1, g_passes_last = 2;
 int g_overlap = 0;
@@ -70,35 +69,8 @@ hipEvent_t side_event() {
     return e;
 }
 
-// Enum-typed arguments come from C callers and may hold any int: read the value without loading it as
-// the enum type (which is undefined for values outside the enumerators), then range-check it.
-template <class E>
-inline int raw_enum(const E& e) {
-    static_assert(sizeof(E) == sizeof(int), "C enums are int-sized in this ABI");
-    int v;
-    std::memcpy(&v, &e, sizeof v);
-    return v;
-}
-inline bool bad_dtype(const atp_dtype& t) { const int v = raw_enum(t); return v != ATP_F32 && v != ATP_BF16; }
-
-inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
-inline bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
-inline size_t esize(atp_dtype t) { return t == ATP_BF16 ? 2 : 4; }
-
-struct Carver {
-    uint8_t* base;
-    size_t off = 0;
-    explicit Carver(void* p) : base(reinterpret_cast<uint8_t*>(p)) {}
-    void* take(size_t bytes) {
-        void* r = base ? base + off : nullptr;
-        off += align_up(bytes);
-        return r;
-    }
-};
-
 // Workspace layout of atp_principal_bases (shared by the query and the call).
 constexpr int KSPLIT_MAX = 8;
-constexpr int NUM_CU = 256;  // compute units of an MI355X
 // The extraction works on padded extents: Lp, dp, rp >= L, d, r are the lengths of its internal rows, filled up with zeros, so that every
 // product runs on the asynchronous bf16 kernel (K a multiple of 64, of 32 with lo planes, rows aligned to 16 bytes) whatever L, d and r
 // are; zero columns of Ω carry through as zero columns of every iterate.  Extents that this kernel takes as they are stay as they are
@@ -172,12 +144,6 @@ BasesWs carve_bases(void* ws, int64_t batch, int64_t L, int64_t d, int64_t r, at
     w.total = c.off;
     return w;
 }
-
-#define ATP_HIP(expr)                               \
-    do {                                            \
-        hipError_t e__ = (expr);                    \
-        if (e__ != hipSuccess) return ATP_ERR_DEVICE; \
-    } while (0)
 
 // C = A · Bᵀ on the backend the storage type calls for: bf16 path -> MFMA kernel (operands bf16,
 // optionally hi+lo planes), fp32 path or shapes the asynchronous kernel does not cover -> strided kernel.
