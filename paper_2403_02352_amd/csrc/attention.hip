@@ -22,24 +22,7 @@
 namespace atp {
 namespace {
 
-__device__ __forceinline__ bf16x8 u4_as_bf16x8(const uint4& u) {
-    union { uint4 u; bf16x8 b; } c;
-    c.u = u;
-    return c.b;
-}
-
 constexpr int QT = 128;  // queries per workgroup (4 waves × 32)
-
-
-// Tiles sit in LDS as plain rows of W 16-byte chunks (W = 16, 8 or 4); position p of row r holds chunk
-// p ^ tile_swz<W>(r).  A 16-byte-per-lane LDS read is served 16 lanes at a time (16 × 16 B = all 64
-// banks), and the 16 lanes of such a group read the same chunk of 16 consecutive rows (in some
-// order): 16/W rows share one 256-byte bank span, so the swizzle counts those spans.
-template <int W>
-__device__ __forceinline__ int tile_swz(int r) {
-    static_assert(W == 16 || W == 8 || W == 4, "row width");
-    return W == 16 ? (r & 15) : W == 8 ? ((r >> 1) & 7) : ((r >> 2) & 3);
-}
 
 // The key/value tiles travel global -> LDS with asynchronous 16-byte copies (no registers), two
 // stages: the copies of tile t+1 fly while tile t is multiplied.  Consecutive lanes of a copy

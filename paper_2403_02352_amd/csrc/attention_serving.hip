@@ -1,6 +1,8 @@
 // Attention of packed sequences over their own tokens, or over the pages of a cache.
 #include "serving.h"
 
+#include <algorithm>
+
 namespace atp {
 namespace {
 
@@ -93,12 +95,440 @@ hipError_t launch_rows(hipStream_t st, const ServeArgs& a, KvSource src) {
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// bf16: tiles of 128 rows and 64 keys on the matrix cores, scores transposed (a row to a lane) as in the attention over principal keys.
+// ---------------------------------------------------------------------------
+constexpr int ROWS = 128, KT = 64;
+
+// 16 bytes a lane from a 64-bit address of its own to LDS (lane q lands at lds + 16·q), untracked by the compiler like copy16_untracked
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16_far(const void* p, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// eight 8-bit codes as bf16, times the power of two whose biased exponent is `byte` (exact, but for values below the normal range)
+__device__ __forceinline__ uint4 expand8(uint2 c, int byte) {
+    const float f = __uint_as_float((uint32_t)byte << 23);
+    union { bf16x2 h[4]; uint4 u; } o;
+    o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c.x, f, false);
+    o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c.x, f, true);
+    o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c.y, f, false);
+    o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c.y, f, true);
+    return o.u;
+}
+
+__device__ __forceinline__ bool any_not_finite(const uint4& u) {
+    const auto word = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
+    return word(u.x) || word(u.y) || word(u.z) || word(u.w);
+}
+
+// DP: head width of the tile; dh <= DP.  COPY: tiles travel to LDS by asynchronous copies (dh == DP, rows in the storage type), else through
+// registers, where codes become bf16 and missing columns zeros.
+template <int DP, int SRC, bool COPY>
+__global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(ServeArgs a, ServePlan p, float c_log2e) {
+    constexpr int CK = DP / 8;            // 16-byte chunks of a row
+    constexpr int NKS = DP / 16, NCT = DP / 32, NT = KT / 32;
+    constexpr int KRPI = 64 / CK;         // rows of a copy instruction
+    constexpr int NKI = KT / KRPI / 4;    // copy instructions of a wave for a tile of keys
+    constexpr bool E4M3 = SRC == KV_PAGED_E4M3;
+    __shared__ __align__(16) uint4 sK[2][KT * CK];
+    __shared__ __align__(16) uint4 sV[2][KT * CK];
+
+    const int hk = blockIdx.x % a.kv_heads;   // consecutive workgroups go to the 8 XCDs in turn: a key head's items share an L2
+    ServeItem it;
+    if (!serve_item<ROWS, KT>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, lh = lane >> 5;
+    const unsigned group = a.heads / a.kv_heads;
+
+    // last key that a row sees (-1: none); rows of a tile see more and more
+    const auto last_key = [&](int row) { return a.causal ? min(it.p0 + (int)((unsigned)row / group), it.kv - 1) : it.kv - 1; };
+    const int row = it.row0 + wave * 32 + l32;
+    const bool live_row = row < it.rows;
+    const int token = it.first + (int)((unsigned)row / group), head = hk * (int)group + (int)((unsigned)row % group);
+    const int lim = live_row ? last_key(row) : -1;
+    const int lim_tile0 = last_key(it.row0), lim_tile1 = last_key(min(it.row0 + ROWS, it.rows) - 1);
+    const int wrow0 = it.row0 + wave * 32;
+    const bool live_wave = wrow0 < it.rows;
+    const int lim_wave0 = live_wave ? last_key(wrow0) : -1, lim_wave1 = live_wave ? last_key(min(wrow0 + 32, it.rows) - 1) : -1;
+
+    // key tiles of this item
+    const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
+    const int kt_end = min((int)((int64_t)it.kt * (it.c + 1) / it.nch), (lim_tile1 + KT) / KT);
+
+    bf16x8 qf[NKS];
+    {
+        const bf16_t* Qp = reinterpret_cast<const bf16_t*>(a.Q) + (int64_t)token * a.ldq + (int64_t)head * a.dh;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            const int c = ks * 16 + lh * 8;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (live_row && (COPY || c < a.dh)) v = *reinterpret_cast<const uint4*>(Qp + c);
+            qf[ks] = u4_as_bf16x8(v);
+        }
+    }
+    f32x16 o[NCT];
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // ---- where keys come from -------------------------------------------------------
+    const int32_t* table = SRC == KV_PACKED ? nullptr : a.table + it.seq * a.max_pages;
+    const int page_mask = (1 << a.page_shift) - 1;
+    // page of key kt·KT + lane, -1 behind the last key
+    const auto page_of = [&](int kt) {
+        const int key = kt * KT + lane;
+        if constexpr (SRC == KV_PACKED) return key < it.kv ? 0 : -1;
+        else return key < it.kv ? table[key >> a.page_shift] : -1;
+    };
+    // first row of the cache that key `kt·KT + r` (its page `pg`) lies in; any row there is for a key that is not
+    const auto cache_row = [&](int kt, int r, int pg) {
+        const int page = pg >= 0 && pg < a.n_pages ? pg : 0;
+        return ((((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * KT + r) & page_mask));
+    };
+    const unsigned wave_s = (unsigned)wave * 1024u;
+    const unsigned lK = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)&sK[0][0]) + wave_s;
+    const unsigned lV = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)&sV[0][0]) + wave_s;
+    constexpr unsigned STAGE = KT * CK * 16;
+    const auto copy_tile = [&](int kt, int pg, int stage) {
+#pragma unroll
+        for (int i = 0; i < NKI; ++i) {
+            const int r = (i * 4 + wave) * KRPI + lane / CK;
+            const int64_t kc = ((lane % CK) ^ tile_swz<CK>(r)) * 8, vc = ((lane % CK) ^ column_swz<DP>(r)) * 8;
+            int64_t kat, vat;
+            if constexpr (SRC == KV_PACKED) {
+                const int64_t t = it.first + min(kt * KT + r, it.kv - 1);   // rows past the end: any row, they weigh nothing
+                kat = t * a.ldk + (int64_t)hk * DP;
+                vat = t * a.ldv + (int64_t)hk * DP;
+            } else {
+                kat = vat = cache_row(kt, r, __shfl(pg, r)) * DP;
+            }
+            copy16_far(reinterpret_cast<const bf16_t*>(a.K) + kat + kc, lK + (unsigned)stage * STAGE + (unsigned)i * 4096u);
+            copy16_far(reinterpret_cast<const bf16_t*>(a.V) + vat + vc, lV + (unsigned)stage * STAGE + (unsigned)i * 4096u);
+        }
+    };
+    constexpr int NL = KT * CK / 256;   // chunks of a thread
+    uint4 kr[COPY ? 1 : NL], vr[COPY ? 1 : NL];
+    int ke[E4M3 ? NL : 1], ve[E4M3 ? NL : 1];
+    const auto load_tile = [&](int kt, int pg) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int c = i * 256 + tid, r = c / CK, f = (c % CK) * 8;
+            const bool inside = f < a.dh;
+            int64_t kat, vat;
+            if constexpr (SRC == KV_PACKED) {
+                const int64_t t = it.first + min(kt * KT + r, it.kv - 1);
+                kat = t * a.ldk + (int64_t)hk * a.dh + f;
+                vat = t * a.ldv + (int64_t)hk * a.dh + f;
+            } else {
+                const int64_t cr = cache_row(kt, r, __shfl(pg, r));
+                if constexpr (E4M3) { ke[i] = a.Ks[cr]; ve[i] = a.Vs[cr]; }
+                kat = vat = cr * a.dh + f;
+            }
+            if constexpr (E4M3) {
+                const uint2 z = make_uint2(0, 0);
+                const uint2 kc = inside ? *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.K) + kat) : z;
+                const uint2 vc = inside ? *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.V) + vat) : z;
+                kr[i] = make_uint4(kc.x, kc.y, 0, 0);
+                vr[i] = make_uint4(vc.x, vc.y, 0, 0);
+            } else {
+                const uint4 z = make_uint4(0, 0, 0, 0);
+                kr[i] = inside ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.K) + kat) : z;
+                vr[i] = inside ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.V) + vat) : z;
+            }
+        }
+    };
+    const auto store_tile = [&](int stage) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int c = i * 256 + tid, r = c / CK, ch = c % CK;
+            uint4 k = kr[i], v = vr[i];
+            if constexpr (E4M3) { k = expand8(make_uint2(k.x, k.y), ke[i]); v = expand8(make_uint2(v.x, v.y), ve[i]); }
+            sK[stage][r * CK + (ch ^ tile_swz<CK>(r))] = k;
+            sV[stage][r * CK + (ch ^ column_swz<DP>(r))] = v;
+        }
+    };
+
+    // S-tile row i holds key perm(i): bits 2 and 3 swapped, so that 8 consecutive accumulator registers of a lane are 8 consecutive keys
+    const int prow = (l32 & ~0xC) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
+    const int pswz = tile_swz<CK>(prow);
+    int v_col[NCT];
+#pragma unroll
+    for (int i = 0; i < NCT; ++i) v_col[i] = column_frag_offset<DP>(lane, 32 * i);
+
+    // alive: keys of the tile that are there; hidden: some row of this wave does not see all of them; spoilt: the values hold something not
+    // finite while some row does not see all of them
+    const auto compute = [&](int kt, const uint4* K, const uint4* V, unsigned long long alive, bool hidden, bool spoilt) {
+        f32x16 s[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[t][v] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) {
+                const bf16x8 kf = u4_as_bf16x8(K[(32 * t + prow) * CK + ((2 * ks + lh) ^ pswz)]);
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
+            }
+        }
+        if (hidden) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int key = 32 * t + 16 * (v >> 3) + 8 * lh + (v & 7);
+                    if (kt * KT + key > lim || !((alive >> key) & 1)) s[t][v] = -INFINITY;
+                }
+        }
+        float mloc = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mloc = fmaxf(mloc, s[t][v]);
+        mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
+        const float m_new = fmaxf(m_run, mloc);
+        // the running maximum settles after a few tiles: rescale only when some row of this wave raised it
+        if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {
+            const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f((m_run - m_new) * c_log2e) : 1.f;
+            l_run *= alpha;
+#pragma unroll
+            for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
+            m_run = m_new;
+        }
+        const float mc = m_run == -INFINITY ? 0.f : m_run * c_log2e;   // no finite score so far: weights of zero, not -inf - -inf
+        float psum = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float pv = __builtin_amdgcn_exp2f(fmaf(s[t][v], c_log2e, -mc));
+                s[t][v] = pv;
+                psum += pv;
+            }
+        l_run += psum;
+        // weights rounded to bf16 for the matrix product; their sum is that of the fp32 values
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                uint4 pu;
+                pu.x = pack_bf2(s[t][8 * tt + 0], s[t][8 * tt + 1]);
+                pu.y = pack_bf2(s[t][8 * tt + 2], s[t][8 * tt + 3]);
+                pu.z = pack_bf2(s[t][8 * tt + 4], s[t][8 * tt + 5]);
+                pu.w = pack_bf2(s[t][8 * tt + 6], s[t][8 * tt + 7]);
+                const bf16x8 pf = u4_as_bf16x8(pu);
+                if (!spoilt) {
+#pragma unroll
+                    for (int i = 0; i < NCT; ++i) {
+                        const bf16x8 vf = read_column_frag<DP>(V, v_col[i] + (32 * t + 16 * tt) * DP * 2);
+                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
+                    }
+                } else {
+                    // zero times infinity is NaN: key by key, and a row takes only what it sees
+#pragma unroll 1
+                    for (int k = 0; k < 16; ++k) {
+                        const int key = 32 * t + 16 * tt + k;
+                        const bool sees = kt * KT + key <= lim && ((alive >> key) & 1);
+                        const uint32_t half = (k >> 3) == lh ? ((k & 1) ? 0xffff0000u : 0xffffu) : 0u;
+                        const int word = (k & 7) >> 1;
+#pragma unroll
+                        for (int i = 0; i < NCT; ++i) {
+                            union { bf16x8 b; uint32_t w[4]; } vf;
+                            vf.b = read_column_frag<DP>(V, v_col[i] + (32 * t + 16 * tt) * DP * 2);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) vf.w[e] &= word == e ? half : 0u;
+                            f32x16 one;
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) one[v] = 0.f;
+                            one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.b, pf, one, 0, 0, 0);
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) o[i][v] += sees ? one[v] : 0.f;
+                        }
+                    }
+                }
+            }
+    };
+
+    int pg = -1, pg_next = -1;
+    if (kt_begin < kt_end) {
+        pg = page_of(kt_begin);
+        if constexpr (COPY) copy_tile(kt_begin, pg, 0);
+        else load_tile(kt_begin, pg);
+    }
+    for (int kt = kt_begin; kt < kt_end; ++kt) {
+        const int stage = (kt - kt_begin) & 1;
+        const unsigned long long alive = __builtin_amdgcn_ballot_w64(pg >= 0 && (SRC == KV_PACKED || pg < a.n_pages));
+        if (kt + 1 < kt_end) pg_next = page_of(kt + 1);
+        if constexpr (COPY) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's copies have landed (the compiler does not count them)
+            __syncthreads();
+            if (kt + 1 < kt_end) copy_tile(kt + 1, pg_next, stage ^ 1);
+        } else {
+            store_tile(stage);
+            __syncthreads();
+            if (kt + 1 < kt_end) load_tile(kt + 1, pg_next);
+        }
+        uint4 *K = sK[stage], *V = sV[stage];
+        // values of keys that are not there become zeros: their weight is zero, but zero times NaN is not
+        if (alive != ~0ull) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int c = i * 256 + tid;
+                if (!((alive >> (c / CK)) & 1)) V[c] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            __syncthreads();
+        }
+        const int last = kt * KT + KT - 1;
+        bool spoilt = false;
+        if (last > lim_tile0) {   // some row does not see all keys
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) bad = bad || any_not_finite(V[i * 256 + tid]);
+            spoilt = __syncthreads_or(bad) != 0;
+        }
+        if (kt * KT <= lim_wave1) compute(kt, K, V, alive, last > lim_wave0 || alive != ~0ull, spoilt);
+        pg = pg_next;
+    }
+
+    const float l_tot = l_run + __shfl_xor(l_run, 32);
+    if (it.nch > 1) {   // one of several chunks: sums as they are, with their maximum
+        if (!live_row) return;
+        const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
+        float* po = p.part_o + at * DP;
+#pragma unroll
+        for (int i = 0; i < NCT; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(po + 32 * i + 8 * g + 4 * lh) = f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+        if (lh == 0) p.part_ml[at] = make_float2(m_run, l_tot);
+        return;
+    }
+    const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
+    __syncthreads();
+    // the output turns in LDS, one stage array a wave, so that a row leaves as 16-byte pieces
+    bf16_t* ob = reinterpret_cast<bf16_t*>(wave < 2 ? sK[wave] : sV[wave - 2]);
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            uint2 w;
+            w.x = pack_bf2(o[i][4 * g + 0] * inv, o[i][4 * g + 1] * inv);
+            w.y = pack_bf2(o[i][4 * g + 2] * inv, o[i][4 * g + 3] * inv);
+            const int piece = (4 * i + g) ^ (l32 & (CK - 1));
+            *reinterpret_cast<uint2*>(ob + l32 * DP + piece * 8 + 4 * lh) = w;
+        }
+#pragma unroll
+    for (int i = 0; i < 32 * CK / 64; ++i) {
+        const int c = i * 64 + lane, qq = c / CK, part = c % CK;
+        const int r = wrow0 + qq;
+        const uint4 v = *reinterpret_cast<const uint4*>(ob + qq * DP + (part ^ (qq & (CK - 1))) * 8);
+        if (r < it.rows && part * 8 < a.dh) {
+            const int64_t t = it.first + (int)((unsigned)r / group), h = hk * (int)group + (int)((unsigned)r % group);
+            *reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(a.O) + t * a.ldo + h * a.dh + part * 8) = v;
+        }
+    }
+}
+
+// Rows whose keys were cut: chunk sums at their common maximum, added in order.  One workgroup per row tile and key head, a thread per row
+// and four features.
+template <typename T, int DP, int ROWS_, int KT_>
+__global__ void __launch_bounds__(256) attn_join_kernel(ServeArgs a, ServePlan p, float c_log2e) {
+    const int hk = blockIdx.x % a.kv_heads;
+    ServeItem it;
+    if (!serve_item<ROWS_, KT_>(a, p, blockIdx.x / a.kv_heads, false, it) || it.nch < 2) return;
+    const unsigned group = a.heads / a.kv_heads;
+    const int end = min(ROWS_, it.rows - it.row0) * (DP / 4);
+    for (int x = threadIdx.x; x < end; x += 256) {
+        const int row = it.row0 + x / (DP / 4), f = 4 * (x % (DP / 4));
+        const int64_t at = (int64_t)hk * p.part_rows + it.part + row;
+        float m = -INFINITY;
+        for (int c = 0; c < it.nch; ++c) m = fmaxf(m, p.part_ml[at + (int64_t)c * it.rows].x);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < it.nch; ++c) {
+            const float2 ml = p.part_ml[at + (int64_t)c * it.rows];
+            const float w = __builtin_amdgcn_exp2f((ml.x - ref) * c_log2e);
+            if (w == 0.f) continue;
+            l = fmaf(ml.y, w, l);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (at + (int64_t)c * it.rows) * DP + f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], w, o[e]);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (f >= a.dh) continue;
+        const int64_t t = it.first + (int)((unsigned)row / group), h = hk * (int)group + (int)((unsigned)row % group);
+        T* Op = reinterpret_cast<T*>(a.O) + t * a.ldo + h * a.dh + f;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(Op) = make_uint2(pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv));
+        else *reinterpret_cast<f32x4*>(Op) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    }
+}
+
+// Items and partial rows that the lengths on the device can lead to, from the sizes that the host knows.  With chunks of at least
+// total / target tiles a cut sequence has fewer than 2·tiles/chunk chunks, so all cut row tiles together have fewer than 2·target.
+ServePlan plan_of(const ServeArgs& a, int64_t rows, int64_t kt, int target, int min_chunk) {
+    ServePlan p;
+    p.target = target;
+    p.min_chunk = min_chunk;
+    const int64_t all_rows = (int64_t)a.tokens * (a.heads / a.kv_heads);
+    const int64_t tiles = all_rows / rows + std::min<int64_t>(a.n_seq, a.tokens);
+    const int64_t cuts = std::min<int64_t>((kt + min_chunk - 1) / min_chunk, 2 * target);
+    p.tiles = (int)tiles;
+    p.items = (int)std::min(tiles + target, tiles * cuts);
+    p.part_rows = cuts < 2 ? 0 : std::min<int64_t>(2 * target * rows, cuts * all_rows);
+    return p;
+}
+
+int padded_width(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
+
+ServePlan plan_bf16(const ServeArgs& a) {
+    const int target = std::max(1, 1024 / a.kv_heads);
+    return plan_of(a, ROWS, ((int64_t)a.max_kv + KT - 1) / KT, target, 4);
+}
+
+size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
+
+template <int DP>
+hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, void* workspace) {
+    ServePlan p = plan_bf16(a);
+    p.part_o = reinterpret_cast<float*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.part_rows * a.kv_heads * DP);
+    const float c = a.scale * 1.4426950408889634f;
+    const int64_t blocks = (int64_t)p.items * a.kv_heads;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks);
+    const bool copy = a.dh == DP;
+    if (src == KV_PACKED) {
+        if (copy) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, true>), grid, dim3(256), 0, st, a, p, c);
+        else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, false>), grid, dim3(256), 0, st, a, p, c);
+    } else if (src == KV_PAGED) {
+        if (copy) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, true>), grid, dim3(256), 0, st, a, p, c);
+        else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, false>), grid, dim3(256), 0, st, a, p, c);
+    } else {
+        hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED_E4M3, false>), grid, dim3(256), 0, st, a, p, c);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.part_rows) return e;
+    hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS, KT>), dim3((unsigned)((int64_t)p.tiles * a.kv_heads)), dim3(256), 0, st, a, p, c);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t serve_attention_workspace(const ServeArgs&, KvSource, int, int64_t) { return 0; }
+size_t serve_attention_workspace(const ServeArgs& a, KvSource, int elem_bytes, int64_t) {
+    if (elem_bytes != 2) return 0;
+    return (part_bytes(a, plan_bf16(a)) + 255) & ~(size_t)255;
+}
 
-hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t, void*) {
-    return elem_bytes == 2 ? launch_rows<bf16_t>(st, a, src) : launch_rows<float>(st, a, src);
+hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t, void* workspace) {
+    if (elem_bytes != 2) return launch_rows<float>(st, a, src);
+    const int dp = padded_width(a.dh);
+    return dp == 64 ? launch_tiles<64>(st, a, src, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, workspace) : launch_tiles<256>(st, a, src, workspace);
 }
 
 }  // namespace atp

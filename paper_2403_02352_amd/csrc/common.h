@@ -44,6 +44,22 @@ __device__ __forceinline__ void copy16_untracked(const void* base, unsigned off_
 }
 #pragma clang diagnostic pop
 
+__device__ __forceinline__ bf16x8 u4_as_bf16x8(const uint4& u) {
+    union { uint4 u; bf16x8 b; } c;
+    c.u = u;
+    return c.b;
+}
+
+// Tiles sit in LDS as plain rows of W 16-byte chunks (W = 32, 16, 8 or 4); position p of row r holds chunk
+// p ^ tile_swz<W>(r).  A 16-byte-per-lane LDS read is served 16 lanes at a time (16 × 16 B = all 64
+// banks), and the 16 lanes of such a group read the same chunk of 16 consecutive rows (in some
+// order): 16/W rows share one 256-byte bank span, so the swizzle counts those spans (a row of 32 chunks has two of its own).
+template <int W>
+__device__ __forceinline__ int tile_swz(int r) {
+    static_assert(W == 32 || W == 16 || W == 8 || W == 4, "row width");
+    return W >= 16 ? (r & 15) : W == 8 ? ((r >> 1) & 7) : ((r >> 2) & 3);
+}
+
 // Fragments of an operand that lies in LDS as it lies in memory, rows of k by columns, come from the transposing LDS read: each
 // of 16 lanes names four consecutive 16-bit elements of a row (lanes 4i .. 4i+3 the 16 columns of row i) and lane c receives
 // column c of the four rows.  Position p of a row of W elements holds 16-byte chunk p ^ column_swz<W>(row), which puts the four

@@ -29,6 +29,16 @@ enum KvSource { KV_PACKED = 0, KV_PAGED = 1, KV_PAGED_E4M3 = 2 };
 hipError_t cache_write_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3);
 hipError_t cache_read_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3);
 
+// How the keys of a call are dealt: about `target` items a key head, of at least `min_chunk` key tiles, partial results of a sequence
+// whose keys are cut go to part_o (rows of floats) and part_ml (maximum and sum of a row).
+struct ServePlan {
+    int target = 1, min_chunk = 1;
+    int tiles = 0, items = 0;   // bounds of the row tiles and of the items of a key head
+    int64_t part_rows = 0;      // bound of the partial rows of a key head
+    float* part_o = nullptr;
+    float2* part_ml = nullptr;
+};
+
 hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new, void* workspace);
 size_t serve_attention_workspace(const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new);
 
@@ -36,6 +46,80 @@ size_t serve_attention_workspace(const ServeArgs& a, KvSource src, int elem_byte
 __device__ __forceinline__ void sequence_rows(const ServeArgs& a, int s, int& first, int& n) {
     first = min(max(a.offsets[s], 0), a.tokens);
     n = max(min(max(a.offsets[s + 1], 0), a.tokens) - first, 0);
+}
+
+// An item of a call's work: a tile of rows (a row is a new token and a query head of the group) of one sequence and chunk c of its nch chunks
+// of key tiles.
+struct ServeItem {
+    int first, n, rows, kv, p0;   // tokens of the sequence; its rows; keys; position of its first new token
+    int seq, row0, c, nch, kt;    // first row of the tile; key tiles of the sequence
+    int64_t part;                 // partial rows of the sequences before this one
+};
+
+// Item w of a key head, the same for every thread of a wave; false behind the last.  Every wave finds it by itself from the lengths on the
+// device: the key tiles that all row tiles go through, over the number of items wanted, give the size of a chunk; then the sequences'
+// items are counted up, 64 sequences at a time.  The host knows none of the lengths, so calls can be captured, and the deal is even for
+// any of them.  With `chunks` off, item w is row tile w.  Row tiles come in descending order: the last ones see the most keys.
+template <int ROWS, int KT>
+__device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& p, int w, bool chunks, ServeItem& it) {
+    const int lane = threadIdx.x & 63;
+    const unsigned group = a.heads / a.kv_heads;
+    int first, n, kv, held;
+    const auto look = [&](int s) {
+        first = n = kv = held = 0;
+        if (s >= a.n_seq) return;
+        sequence_rows(a, s, first, n);
+        held = a.length ? max(a.length[s], 0) : n;
+        kv = min(held, a.max_kv);
+    };
+    const auto row_tiles = [&] { return (int)(((unsigned)n * group + ROWS - 1) / ROWS); };
+    const auto key_tiles = [&] { return max((kv + KT - 1) / KT, 1); };
+    long long total = 0;
+    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+        look(s0 + lane);
+        total += (long long)row_tiles() * key_tiles();
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
+    const long long even = (total + p.target - 1) / p.target;
+    const int chunk = (int)min(max(even, (long long)p.min_chunk), (long long)(1 << 30));
+    int before = 0;
+    long long part = 0;
+    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+        if (a.n_seq > 64) look(s0 + lane);
+        const int kt = key_tiles(), nch = (kt + chunk - 1) / chunk, rt = row_tiles();
+        const int mine = chunks ? rt * nch : rt;
+        const long long mine_part = nch > 1 ? (long long)((unsigned)n * group) * nch : 0;
+        int upto = mine;
+        long long upto_part = mine_part;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int x = __shfl_up(upto, off);
+            const long long y = __shfl_up(upto_part, off);
+            if (lane >= off) { upto += x; upto_part += y; }
+        }
+        const unsigned long long behind = __builtin_amdgcn_ballot_w64(before + upto > w);
+        if (behind) {
+            const int at = __builtin_ctzll(behind);
+            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            it.first = of(first); it.n = of(n); it.kv = of(kv); it.p0 = of(held) - it.n;
+            it.rows = it.n * (int)group;
+            it.kt = of(kt);
+            it.seq = s0 + at;
+            it.nch = of(nch);
+            const int local = w - before - of(upto - mine), per = chunks ? it.nch : 1;
+            it.row0 = (of(rt) - 1 - local / per) * ROWS;
+            it.c = local % per;
+            const long long pb = part + upto_part - mine_part;
+            it.part = (long long)(((unsigned long long)(unsigned)of((int)(pb >> 32)) << 32) | (unsigned)of((int)pb));
+            // (offsets that decrease can count more rows than there are: no item for what the grid and the workspace do not hold)
+            return local >= 0 && local < of(mine) && (it.nch == 1 || it.part + (int64_t)it.rows * it.nch <= p.part_rows);
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+        const long long last = __shfl(upto_part, 63);
+        part += last;
+    }
+    return false;
 }
 
 // The sequence that owns `token` (-1: none), found by a whole wave: 64 offsets at a time, the interval they leave is cut in 64 again.
