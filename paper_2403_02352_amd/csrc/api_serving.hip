@@ -34,7 +34,7 @@ atp_status take_cache(const atp_cache* c, const atp_batch* b, const atp_dtype& t
 
 // a packed tensor: rows of `row` elements, `ld` apart
 bool bad_rows(const void* p, int64_t ld, int64_t row, atp_dtype t) {
-    return !p || !aligned16(p) || ld < row || ld > (int64_t(1) << 40) || (ld * (int64_t)esize(t)) % 16;
+    return !p || !aligned16(p) || ld < row || ld > (1 << 24) || (ld * (int64_t)esize(t)) % 16;
 }
 
 KvSource source_of(const atp_cache* c) { return raw_enum(c->type) == ATP_CACHE_E4M3 ? KV_PAGED_E4M3 : KV_PAGED; }

@@ -12,35 +12,27 @@ __device__ __forceinline__ float element(const T* p) {
     else return *p;
 }
 
-// One wave per token and query head, key after key: features lane, lane + 64, ... with one pass of running maximum and sum.
+// One row over keys kt0 .. kt1-1, key after key, by a whole wave: features lane, lane + 64, ... with one pass of running maximum and sum.
+// No key that the row does not see is touched.
+struct RowSum { float o[4], m, l; };
+
 template <typename T, int SRC>
-__global__ void __launch_bounds__(256) attn_rows_kernel(ServeArgs a) {
+__device__ __forceinline__ RowSum attend_row(const ServeArgs& a, int seq, int first, int hk, const T* Qp, int key0, int key1) {
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int token = __builtin_amdgcn_readfirstlane((int)(w / a.heads)), h = __builtin_amdgcn_readfirstlane((int)(w % a.heads));
-    if (token >= a.tokens) return;
-    const int s = sequence_of(a, token);
-    if (s < 0) return;
-    int first, n;
-    sequence_rows(a, s, first, n);
-    const int held = SRC == KV_PACKED ? n : max(a.length[s], 0);
-    const int pos = held - n + (token - first);
-    int keys = SRC == KV_PACKED ? n : min(held, a.max_kv);
-    if (a.causal) keys = min(keys, pos + 1);
-    const int hk = h / (a.heads / a.kv_heads);
-    float qv[4], ov[4];
-    const T* Qp = reinterpret_cast<const T*>(a.Q) + (int64_t)token * a.ldq + (int64_t)h * a.dh;
+    float qv[4];
+    RowSum r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         qv[i] = lane + 64 * i < a.dh ? element(Qp + lane + 64 * i) : 0.f;
-        ov[i] = 0.f;
+        r.o[i] = 0.f;
     }
-    float m_run = -INFINITY, l_run = 0.f;
-    for (int j = 0; j < keys; ++j) {
+    r.m = -INFINITY;
+    r.l = 0.f;
+    for (int j = key0; j < key1; ++j) {
         float kv[4], vv[4];
         int64_t at = 0;
         if constexpr (SRC != KV_PACKED) {
-            const int page = a.table[s * a.max_pages + (j >> a.page_shift)];
+            const int page = a.table[seq * a.max_pages + (j >> a.page_shift)];
             if (page < 0 || page >= a.n_pages) continue;
             at = (((int64_t)page * a.kv_heads + hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
         }
@@ -67,22 +59,65 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(ServeArgs a) {
         for (int i = 0; i < 4; ++i) sc = fmaf(qv[i], kv[i], sc);
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) sc += __shfl_xor(sc, off);
-        sc *= a.scale;
-        const float m_new = fmaxf(m_run, sc), m_ref = m_new == -INFINITY ? 0.f : m_new;
-        const float keep = expf(m_run - m_ref), p = expf(sc - m_ref);
-        l_run = l_run * keep + p;
-        m_run = m_new;
+        const float m_new = fmaxf(r.m, sc), m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float keep = expf((r.m - m_ref) * a.scale), p = expf((sc - m_ref) * a.scale);
+        r.l = r.l * keep + p;
+        r.m = m_new;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ov[i] = fmaf(p, vv[i], ov[i] * keep);
+        for (int i = 0; i < 4; ++i) r.o[i] = fmaf(p, vv[i], r.o[i] * keep);
     }
-    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-    T* Op = reinterpret_cast<T*>(a.O) + (int64_t)token * a.ldo + (int64_t)h * a.dh;
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(T* Op, const RowSum& r, int dh) {
+    const int lane = threadIdx.x & 63;
+    const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < a.dh) {
-            if constexpr (sizeof(T) == 2) Op[lane + 64 * i] = f2bf(ov[i] * inv);
-            else Op[lane + 64 * i] = ov[i] * inv;
+        if (lane + 64 * i < dh) {
+            if constexpr (sizeof(T) == 2) Op[lane + 64 * i] = f2bf(r.o[i] * inv);
+            else Op[lane + 64 * i] = r.o[i] * inv;
         }
+}
+
+// The rows of an item, wave by wave, where a value that is not finite stands at a key that some of them do not see: a product of tiles
+// would carry it into every row (zero times infinity is NaN).
+template <typename T, int SRC, int ROWS_>
+__device__ __forceinline__ void attend_item_by_rows(const ServeArgs& a, const ServePlan& p, const ServeItem& it, int hk, int key0, int key1, int dp) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned group = a.heads / a.kv_heads;
+    for (int row = it.row0 + wave; row < min(it.row0 + ROWS_, it.rows); row += 4) {
+        const int i = (int)((unsigned)row / group), h = hk * (int)group + (int)((unsigned)row % group);
+        const int keys = min(a.causal ? min(it.p0 + i + 1, it.kv) : it.kv, key1);
+        const RowSum r = attend_row<T, SRC>(a, it.seq, it.first, hk, reinterpret_cast<const T*>(a.Q) + (int64_t)(it.first + i) * a.ldq + (int64_t)h * a.dh, key0, keys);
+        if (it.nch == 1) {
+            store_row(reinterpret_cast<T*>(a.O) + (int64_t)(it.first + i) * a.ldo + (int64_t)h * a.dh, r, a.dh);
+        } else {
+            const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+                if (lane + 64 * f < dp) p.part_o[at * dp + lane + 64 * f] = r.o[f];
+            if (lane == 0) p.part_ml[at] = make_float2(r.m, r.l);
+        }
+    }
+}
+
+template <typename T, int SRC>
+__global__ void __launch_bounds__(256) attn_rows_kernel(ServeArgs a) {
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int token = __builtin_amdgcn_readfirstlane((int)(w / a.heads)), h = __builtin_amdgcn_readfirstlane((int)(w % a.heads));
+    if (token >= a.tokens) return;
+    const int s = sequence_of(a, token);
+    if (s < 0) return;
+    int first, n;
+    sequence_rows(a, s, first, n);
+    const int held = SRC == KV_PACKED ? n : max(a.length[s], 0);
+    const int pos = held - n + (token - first);
+    int keys = SRC == KV_PACKED ? n : min(held, a.max_kv);
+    if (a.causal) keys = min(keys, pos + 1);
+    const RowSum r = attend_row<T, SRC>(a, s, first, h / (a.heads / a.kv_heads), reinterpret_cast<const T*>(a.Q) + (int64_t)token * a.ldq + (int64_t)h * a.dh, 0, keys);
+    store_row(reinterpret_cast<T*>(a.O) + (int64_t)token * a.ldo + (int64_t)h * a.dh, r, a.dh);
 }
 
 template <typename T>
@@ -194,21 +229,52 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     const unsigned lK = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)&sK[0][0]) + wave_s;
     const unsigned lV = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)&sV[0][0]) + wave_s;
     constexpr unsigned STAGE = KT * CK * 16;
+    // A tile whose rows follow each other (packed, or within one page) is copied from a scalar base with lane offsets that stay the same;
+    // pages shorter than a tile give every lane an address of its own.
+    const bool whole = SRC == KV_PACKED || a.page_shift >= 6;
+    const unsigned kb = SRC == KV_PACKED ? (unsigned)a.ldk * 2u : DP * 2u, vb = SRC == KV_PACKED ? (unsigned)a.ldv * 2u : DP * 2u;
+    unsigned k_ofs[NKI], v_ofs[NKI];
+#pragma unroll
+    for (int i = 0; i < NKI; ++i) {
+        const int r = (i * 4 + wave) * KRPI + lane / CK;
+        k_ofs[i] = (unsigned)r * kb + (unsigned)((lane % CK) ^ tile_swz<CK>(r)) * 16u;
+        v_ofs[i] = (unsigned)r * vb + (unsigned)((lane % CK) ^ column_swz<DP>(r)) * 16u;
+    }
+    const bf16_t* Kh = reinterpret_cast<const bf16_t*>(a.K) + (SRC == KV_PACKED ? (int64_t)it.first * a.ldk + (int64_t)hk * DP : 0);
+    const bf16_t* Vh = reinterpret_cast<const bf16_t*>(a.V) + (SRC == KV_PACKED ? (int64_t)it.first * a.ldv + (int64_t)hk * DP : 0);
     const auto copy_tile = [&](int kt, int pg, int stage) {
+        const unsigned lk = lK + (unsigned)stage * STAGE, lv = lV + (unsigned)stage * STAGE;
+        if (whole && (SRC != KV_PACKED || kt * KT + KT <= it.kv)) {
+            const bf16_t *K = Kh, *V = Vh;
+            if constexpr (SRC == KV_PACKED) {
+                K += (int64_t)(kt * KT) * a.ldk;
+                V += (int64_t)(kt * KT) * a.ldv;
+            } else {
+                const int64_t r = cache_row(kt, 0, __builtin_amdgcn_readfirstlane(pg)) * DP;
+                K += r;
+                V += r;
+            }
+#pragma unroll
+            for (int i = 0; i < NKI; ++i) {
+                copy16_untracked(K, k_ofs[i], lk + (unsigned)i * 4096u);
+                copy16_untracked(V, v_ofs[i], lv + (unsigned)i * 4096u);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NKI; ++i) {
             const int r = (i * 4 + wave) * KRPI + lane / CK;
-            const int64_t kc = ((lane % CK) ^ tile_swz<CK>(r)) * 8, vc = ((lane % CK) ^ column_swz<DP>(r)) * 8;
+            const unsigned kc = k_ofs[i] - (unsigned)r * kb, vc = v_ofs[i] - (unsigned)r * vb;
             int64_t kat, vat;
             if constexpr (SRC == KV_PACKED) {
-                const int64_t t = it.first + min(kt * KT + r, it.kv - 1);   // rows past the end: any row, they weigh nothing
-                kat = t * a.ldk + (int64_t)hk * DP;
-                vat = t * a.ldv + (int64_t)hk * DP;
+                const int64_t t = min(kt * KT + r, it.kv - 1);   // rows past the end: any row, they weigh nothing
+                kat = t * a.ldk;
+                vat = t * a.ldv;
             } else {
                 kat = vat = cache_row(kt, r, __shfl(pg, r)) * DP;
             }
-            copy16_far(reinterpret_cast<const bf16_t*>(a.K) + kat + kc, lK + (unsigned)stage * STAGE + (unsigned)i * 4096u);
-            copy16_far(reinterpret_cast<const bf16_t*>(a.V) + vat + vc, lV + (unsigned)stage * STAGE + (unsigned)i * 4096u);
+            copy16_far(reinterpret_cast<const uint8_t*>(Kh + kat) + kc, lk + (unsigned)i * 4096u);
+            copy16_far(reinterpret_cast<const uint8_t*>(Vh + vat) + vc, lv + (unsigned)i * 4096u);
         }
     };
     constexpr int NL = KT * CK / 256;   // chunks of a thread
@@ -260,9 +326,8 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
 #pragma unroll
     for (int i = 0; i < NCT; ++i) v_col[i] = column_frag_offset<DP>(lane, 32 * i);
 
-    // alive: keys of the tile that are there; hidden: some row of this wave does not see all of them; spoilt: the values hold something not
-    // finite while some row does not see all of them
-    const auto compute = [&](int kt, const uint4* K, const uint4* V, unsigned long long alive, bool hidden, bool spoilt) {
+    // alive: keys of the tile that are there; hidden: some row of this wave does not see all of them
+    const auto compute = [&](int kt, const uint4* K, const uint4* V, unsigned long long alive, bool hidden) {
         f32x16 s[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -322,39 +387,16 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
                 pu.z = pack_bf2(s[t][8 * tt + 4], s[t][8 * tt + 5]);
                 pu.w = pack_bf2(s[t][8 * tt + 6], s[t][8 * tt + 7]);
                 const bf16x8 pf = u4_as_bf16x8(pu);
-                if (!spoilt) {
 #pragma unroll
-                    for (int i = 0; i < NCT; ++i) {
-                        const bf16x8 vf = read_column_frag<DP>(V, v_col[i] + (32 * t + 16 * tt) * DP * 2);
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
-                    }
-                } else {
-                    // zero times infinity is NaN: key by key, and a row takes only what it sees
-#pragma unroll 1
-                    for (int k = 0; k < 16; ++k) {
-                        const int key = 32 * t + 16 * tt + k;
-                        const bool sees = kt * KT + key <= lim && ((alive >> key) & 1);
-                        const uint32_t half = (k >> 3) == lh ? ((k & 1) ? 0xffff0000u : 0xffffu) : 0u;
-                        const int word = (k & 7) >> 1;
-#pragma unroll
-                        for (int i = 0; i < NCT; ++i) {
-                            union { bf16x8 b; uint32_t w[4]; } vf;
-                            vf.b = read_column_frag<DP>(V, v_col[i] + (32 * t + 16 * tt) * DP * 2);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) vf.w[e] &= word == e ? half : 0u;
-                            f32x16 one;
-#pragma unroll
-                            for (int v = 0; v < 16; ++v) one[v] = 0.f;
-                            one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.b, pf, one, 0, 0, 0);
-#pragma unroll
-                            for (int v = 0; v < 16; ++v) o[i][v] += sees ? one[v] : 0.f;
-                        }
-                    }
+                for (int i = 0; i < NCT; ++i) {
+                    const bf16x8 vf = read_column_frag<DP>(V, v_col[i] + (32 * t + 16 * tt) * DP * 2);
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
                 }
             }
     };
 
     int pg = -1, pg_next = -1;
+    bool spoilt = false;   // the values hold something not finite where some row does not see all of them
     if (kt_begin < kt_end) {
         pg = page_of(kt_begin);
         if constexpr (COPY) copy_tile(kt_begin, pg, 0);
@@ -384,15 +426,20 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
             __syncthreads();
         }
         const int last = kt * KT + KT - 1;
-        bool spoilt = false;
         if (last > lim_tile0) {   // some row does not see all keys
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < NL; ++i) bad = bad || any_not_finite(V[i * 256 + tid]);
             spoilt = __syncthreads_or(bad) != 0;
+            if (spoilt) break;
         }
-        if (kt * KT <= lim_wave1) compute(kt, K, V, alive, last > lim_wave0 || alive != ~0ull, spoilt);
+        if (kt * KT <= lim_wave1) compute(kt, K, V, alive, last > lim_wave0 || alive != ~0ull);
         pg = pg_next;
+    }
+    if (spoilt) {
+        if constexpr (COPY) __builtin_amdgcn_s_waitcnt(0x0F70);   // no copy is left in flight
+        attend_item_by_rows<bf16_t, SRC, ROWS>(a, p, it, hk, kt_begin * KT, kt_end * KT, DP);
+        return;
     }
 
     const float l_tot = l_run + __shfl_xor(l_run, 32);
