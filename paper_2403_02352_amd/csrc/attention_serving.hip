@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
             __syncthreads();
         }
         const int last = kt * KT + KT - 1;
-        if (last > lim_tile0) {   // some row does not see all keys
+        if (min(last, it.kv - 1) > lim_tile0) {   // some row does not see all keys
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < NL; ++i) bad = bad || any_not_finite(V[i * 256 + tid]);
@@ -481,6 +481,260 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     }
 }
 
+// ---------------------------------------------------------------------------
+// bf16, few rows: tiles of 32 rows and 32 keys, the key tiles of an item dealt to four waves that meet at the end.  For the single tokens of a
+// step the keys are read once whatever is done with them, so what counts is bytes in flight: nothing but the wave's own loads holds it up (no
+// barrier in the loop), page numbers are fetched two tiles ahead, keys one tile ahead into the registers that the score product
+// takes them from (a lane's 16 bytes of a key's row), values one tile ahead into registers, from where they pass through a tile of LDS of the wave's own that
+// the transposing read turns.
+// ---------------------------------------------------------------------------
+constexpr int ROWS_S = 32, KT_S = 32;
+
+template <int DP, int SRC>
+__global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(ServeArgs a, ServePlan p, float c_log2e) {
+    constexpr bool E4M3 = SRC == KV_PAGED_E4M3;
+    constexpr int CK = DP / 8, NKS = DP / 16, NCT = DP / 32;
+    constexpr int EPL = E4M3 ? 16 : 8;          // elements of a 16-byte load
+    constexpr int NK = DP / (2 * EPL);          // loads of a lane for its half of a key row
+    constexpr int LPR = DP / EPL;               // lanes to a value row
+    constexpr int NV = KT_S * LPR / 64;         // value loads of a lane
+    __shared__ __align__(16) uint4 sV[4][KT_S * CK];
+    __shared__ float2 sML[2][64];
+    __shared__ int sSpoilt;
+
+    const int hk = blockIdx.x % a.kv_heads;
+    ServeItem it;
+    if (!serve_item<ROWS_S, KT_S>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, lh = lane >> 5;
+    const unsigned group = a.heads / a.kv_heads;
+    const auto last_key = [&](int row) { return a.causal ? min(it.p0 + (int)((unsigned)row / group), it.kv - 1) : it.kv - 1; };
+    const int row = it.row0 + l32;
+    const bool live_row = row < it.rows;
+    const int64_t token = it.first + (int)((unsigned)row / group), head = hk * (int)group + (int)((unsigned)row % group);
+    const int lim = live_row ? last_key(row) : -1;
+    const int lim0 = last_key(it.row0), lim1 = last_key(min(it.row0 + ROWS_S, it.rows) - 1);
+    const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
+    const int kt_end = min((int)((int64_t)it.kt * (it.c + 1) / it.nch), (lim1 + KT_S) / KT_S);
+    if (tid == 0) sSpoilt = 0;
+    __syncthreads();
+
+    // features of k-step ks that lane half lh multiplies: any order, as long as queries and keys agree
+    const auto feature = [&](int ks) { return E4M3 ? 32 * (ks >> 1) + 16 * lh + 8 * (ks & 1) : 16 * ks + 8 * lh; };
+    bf16x8 qf[NKS];
+    {
+        const bf16_t* Qp = reinterpret_cast<const bf16_t*>(a.Q) + token * a.ldq + head * a.dh;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (live_row && feature(ks) < a.dh) v = *reinterpret_cast<const uint4*>(Qp + feature(ks));
+            qf[ks] = u4_as_bf16x8(v);
+        }
+    }
+    f32x16 o[NCT];
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    const int32_t* table = SRC == KV_PACKED ? nullptr : a.table + it.seq * a.max_pages;
+    const int page_mask = (1 << a.page_shift) - 1;
+    const int prow = (l32 & ~0xC) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);   // the key of this lane's row of the score product
+    const auto page_of = [&](int kt) {   // of key kt·KT_S + l32, -1 behind the last key
+        const int key = kt * KT_S + l32;
+        if (kt >= kt_end || key >= it.kv) return -1;
+        if constexpr (SRC == KV_PACKED) return 0;
+        else return table[key >> a.page_shift];
+    };
+    const bool whole = SRC == KV_PACKED || a.page_shift >= 5;   // the rows of a tile follow each other
+    // element offset of key row r of a tile; any row for a key that is not there
+    const auto row_at = [&](int kt, int r, int pg, int64_t ld) -> int64_t {
+        if constexpr (SRC == KV_PACKED) return (int64_t)(it.first + min(kt * KT_S + r, it.kv - 1)) * ld + (int64_t)hk * a.dh;
+        const int pr = whole ? __builtin_amdgcn_readfirstlane(pg) : __shfl(pg, r);
+        const int page = pr >= 0 && pr < a.n_pages ? pr : 0;
+        return (((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * KT_S + r) & page_mask);   // row of the cache
+    };
+    const bool even = !E4M3 || a.dh % 16 == 0;
+    const auto piece = [&](const void* base, int64_t at, int f) {   // 16 bytes of a row, zeros past its end
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if constexpr (E4M3) {
+            const uint8_t* q = reinterpret_cast<const uint8_t*>(base) + at * a.dh + f;
+            if (even) { if (f < a.dh) v = *reinterpret_cast<const uint4*>(q); }
+            else {
+                if (f < a.dh) { const uint2 x = *reinterpret_cast<const uint2*>(q); v.x = x.x; v.y = x.y; }
+                if (f + 8 < a.dh) { const uint2 x = *reinterpret_cast<const uint2*>(q + 8); v.z = x.x; v.w = x.y; }
+            }
+        } else {
+            const bf16_t* q = reinterpret_cast<const bf16_t*>(base) + (SRC == KV_PACKED ? at : at * a.dh) + f;
+            if (f < a.dh) v = *reinterpret_cast<const uint4*>(q);
+        }
+        return v;
+    };
+    uint4 kr[NK], vr[NV];
+    int ke = 0, ve[E4M3 ? NV : 1];
+    const auto load_keys = [&](int kt, int pg) {
+        const int64_t at = row_at(kt, prow, pg, a.ldk);
+        if constexpr (E4M3) ke = a.Ks[at];
+#pragma unroll
+        for (int i = 0; i < NK; ++i) kr[i] = piece(a.K, at, 2 * EPL * i + EPL * lh);
+    };
+    const auto load_values = [&](int kt, int pg) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int r = i * (64 / LPR) + lane / LPR;
+            const int64_t at = row_at(kt, r, pg, a.ldv);
+            if constexpr (E4M3) ve[i] = a.Vs[at];
+            vr[i] = piece(a.V, at, EPL * (lane % LPR));
+        }
+    };
+    uint4* V = sV[wave];
+    int v_col[NCT];
+#pragma unroll
+    for (int i = 0; i < NCT; ++i) v_col[i] = column_frag_offset<DP>(lane, 32 * i);
+    const bool partial = lim0 < it.kv - 1;   // some row does not see all keys of the sequence
+    bool spoilt = false;
+
+    int kt = kt_begin + wave;
+    int pg0 = page_of(kt), pg1 = page_of(kt + 4);
+    if (kt < kt_end) { load_keys(kt, pg0); load_values(kt, pg0); }
+    for (; kt < kt_end; kt += 4) {
+        const unsigned alive = (unsigned)__builtin_amdgcn_ballot_w64(pg0 >= 0 && (SRC == KV_PACKED || pg0 < a.n_pages));
+        const int pg2 = page_of(kt + 8);
+        f32x16 s;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if constexpr (E4M3) {
+                const bf16x8 k0 = u4_as_bf16x8(expand8(make_uint2(kr[i].x, kr[i].y), ke)), k1 = u4_as_bf16x8(expand8(make_uint2(kr[i].z, kr[i].w), ke));
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qf[2 * i], s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qf[2 * i + 1], s, 0, 0, 0);
+            } else {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u4_as_bf16x8(kr[i]), qf[i], s, 0, 0, 0);
+            }
+        }
+        if (kt + 4 < kt_end) load_keys(kt + 4, pg1);
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int r = i * (64 / LPR) + lane / LPR, f = lane % LPR;
+            const bool there = (alive >> r) & 1;   // a weight of zero does not take NaN away: values of keys that are not there are zeros
+            if constexpr (E4M3) {
+                uint4 lo = expand8(make_uint2(vr[i].x, vr[i].y), ve[i]), hi = expand8(make_uint2(vr[i].z, vr[i].w), ve[i]);
+                if (!there) lo = hi = make_uint4(0, 0, 0, 0);
+                if (partial) bad = bad || any_not_finite(lo) || any_not_finite(hi);
+                V[r * CK + ((2 * f) ^ column_swz<DP>(r))] = lo;
+                V[r * CK + ((2 * f + 1) ^ column_swz<DP>(r))] = hi;
+            } else {
+                const uint4 v = there ? vr[i] : make_uint4(0, 0, 0, 0);
+                if (partial) bad = bad || any_not_finite(v);
+                V[r * CK + (f ^ column_swz<DP>(r))] = v;
+            }
+        }
+        if (kt + 4 < kt_end) load_values(kt + 4, pg1);
+        if (min(kt * KT_S + KT_S, it.kv) - 1 > lim0 && __builtin_amdgcn_ballot_w64(bad) != 0) spoilt = true;
+        if (kt * KT_S + KT_S - 1 > lim0 || alive != ~0u) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int key = 16 * (v >> 3) + 8 * lh + (v & 7);
+                if (kt * KT_S + key > lim || !((alive >> key) & 1)) s[v] = -INFINITY;
+            }
+        }
+        float mloc = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mloc = fmaxf(mloc, s[v]);
+        mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
+        const float m_new = fmaxf(m_run, mloc);
+        if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {
+            const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f((m_run - m_new) * c_log2e) : 1.f;
+            l_run *= alpha;
+#pragma unroll
+            for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
+            m_run = m_new;
+        }
+        const float mc = m_run == -INFINITY ? 0.f : m_run * c_log2e;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c_log2e, -mc));
+            l_run += s[v];
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            uint4 pu;   // weights rounded to bf16 for the matrix product
+            pu.x = pack_bf2(s[8 * tt + 0], s[8 * tt + 1]);
+            pu.y = pack_bf2(s[8 * tt + 2], s[8 * tt + 3]);
+            pu.z = pack_bf2(s[8 * tt + 4], s[8 * tt + 5]);
+            pu.w = pack_bf2(s[8 * tt + 6], s[8 * tt + 7]);
+            const bf16x8 pf = u4_as_bf16x8(pu);
+#pragma unroll
+            for (int i = 0; i < NCT; ++i) {
+                const bf16x8 vf = read_column_frag<DP>(V, v_col[i] + 16 * tt * DP * 2);
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
+            }
+        }
+        pg0 = pg1;
+        pg1 = pg2;
+    }
+    if (spoilt && lane == 0) sSpoilt = 1;
+    __syncthreads();
+    if (sSpoilt) {
+        attend_item_by_rows<bf16_t, SRC, ROWS_S>(a, p, it, hk, kt_begin * KT_S, kt_end * KT_S, DP);
+        return;
+    }
+    l_run += __shfl_xor(l_run, 32);
+    // waves 2 and 3 hand their sums to waves 0 and 1, wave 1 to wave 0, at the larger maximum
+    float* share = reinterpret_cast<float*>(sV);
+    constexpr int PER = NCT * 16 * 64;
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) share[(wave - half) * PER + (16 * i + v) * 64 + lane] = o[i][v];
+            sML[wave - half][lane] = make_float2(m_run, l_run);
+        }
+        __syncthreads();
+        if (wave < half) {
+            const float2 ml = sML[wave][lane];
+            const float m_all = fmaxf(m_run, ml.x), ref = m_all == -INFINITY ? 0.f : m_all;
+            const float f0 = __builtin_amdgcn_exp2f((m_run - ref) * c_log2e), f1 = __builtin_amdgcn_exp2f((ml.x - ref) * c_log2e);
+            l_run = l_run * f0 + ml.y * f1;
+            m_run = m_all;
+#pragma unroll
+            for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[i][v] = fmaf(share[wave * PER + (16 * i + v) * 64 + lane], f1, o[i][v] * f0);
+        }
+        __syncthreads();
+    }
+    if (wave || !live_row) return;
+    if (it.nch > 1) {
+        const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
+        float* po = p.part_o + at * DP;
+#pragma unroll
+        for (int i = 0; i < NCT; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(po + 32 * i + 8 * g + 4 * lh) = f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+        if (lh == 0) p.part_ml[at] = make_float2(m_run, l_run);
+        return;
+    }
+    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+    bf16_t* Op = reinterpret_cast<bf16_t*>(a.O) + token * a.ldo + head * a.dh;
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int f = 32 * i + 8 * g + 4 * lh;
+            if (f < a.dh)
+                *reinterpret_cast<uint2*>(Op + f) = make_uint2(pack_bf2(o[i][4 * g] * inv, o[i][4 * g + 1] * inv), pack_bf2(o[i][4 * g + 2] * inv, o[i][4 * g + 3] * inv));
+        }
+}
+
 // Rows whose keys were cut: chunk sums at their common maximum, added in order.  One workgroup per row tile and key head, a thread per row
 // and four features.
 template <typename T, int DP, int ROWS_, int KT_>
@@ -533,16 +787,23 @@ ServePlan plan_of(const ServeArgs& a, int64_t rows, int64_t kt, int target, int 
 
 int padded_width(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 
-ServePlan plan_bf16(const ServeArgs& a) {
+// Few rows a sequence (by what the caller says, else on average): the kernel of 32 rows.
+bool few_rows(const ServeArgs& a, int64_t max_new) {
+    const int64_t group = a.heads / a.kv_heads;
+    const int64_t rows = max_new > 0 ? std::min<int64_t>(max_new, a.tokens) * group : ((int64_t)a.tokens + a.n_seq - 1) / a.n_seq * group;
+    return rows <= ROWS_S;
+}
+
+ServePlan plan_bf16(const ServeArgs& a, bool few) {
     const int target = std::max(1, 1024 / a.kv_heads);
-    return plan_of(a, ROWS, ((int64_t)a.max_kv + KT - 1) / KT, target, 4);
+    return few ? plan_of(a, ROWS_S, ((int64_t)a.max_kv + KT_S - 1) / KT_S, target, 8) : plan_of(a, ROWS, ((int64_t)a.max_kv + KT - 1) / KT, target, 4);
 }
 
 size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
 
 template <int DP>
-hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, void* workspace) {
-    ServePlan p = plan_bf16(a);
+hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool few, void* workspace) {
+    ServePlan p = plan_bf16(a, few);
     p.part_o = reinterpret_cast<float*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.part_rows * a.kv_heads * DP);
     const float c = a.scale * 1.4426950408889634f;
@@ -550,7 +811,11 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, void* 
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
     const bool copy = a.dh == DP;
-    if (src == KV_PACKED) {
+    if (few) {
+        if (src == KV_PACKED) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED>), grid, dim3(256), 0, st, a, p, c);
+        else if (src == KV_PAGED) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED>), grid, dim3(256), 0, st, a, p, c);
+        else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a, p, c);
+    } else if (src == KV_PACKED) {
         if (copy) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, true>), grid, dim3(256), 0, st, a, p, c);
         else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, false>), grid, dim3(256), 0, st, a, p, c);
     } else if (src == KV_PAGED) {
@@ -561,21 +826,24 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, void* 
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part_rows) return e;
-    hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS, KT>), dim3((unsigned)((int64_t)p.tiles * a.kv_heads)), dim3(256), 0, st, a, p, c);
+    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads));
+    if (few) hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS_S, KT_S>), join, dim3(256), 0, st, a, p, c);
+    else hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS, KT>), join, dim3(256), 0, st, a, p, c);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t serve_attention_workspace(const ServeArgs& a, KvSource, int elem_bytes, int64_t) {
+size_t serve_attention_workspace(const ServeArgs& a, KvSource, int elem_bytes, int64_t max_new) {
     if (elem_bytes != 2) return 0;
-    return (part_bytes(a, plan_bf16(a)) + 255) & ~(size_t)255;
+    return (part_bytes(a, plan_bf16(a, few_rows(a, max_new))) + 255) & ~(size_t)255;
 }
 
-hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t, void* workspace) {
+hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new, void* workspace) {
     if (elem_bytes != 2) return launch_rows<float>(st, a, src);
     const int dp = padded_width(a.dh);
-    return dp == 64 ? launch_tiles<64>(st, a, src, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, workspace) : launch_tiles<256>(st, a, src, workspace);
+    const bool few = few_rows(a, max_new);
+    return dp == 64 ? launch_tiles<64>(st, a, src, few, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, few, workspace) : launch_tiles<256>(st, a, src, few, workspace);
 }
 
 }  // namespace atp
