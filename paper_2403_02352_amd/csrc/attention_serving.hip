@@ -155,8 +155,8 @@ __device__ __forceinline__ uint4 expand8(uint2 c, int byte) {
 }
 
 __device__ __forceinline__ bool any_not_finite(const uint4& u) {
-    const auto word = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
-    return word(u.x) || word(u.y) || word(u.z) || word(u.w);
+    const auto word = [](uint32_t x) { return ((x & 0x7f80u) == 0x7f80u) | ((x & 0x7f800000u) == 0x7f800000u); };
+    return word(u.x) | word(u.y) | word(u.z) | word(u.w);
 }
 
 // DP: head width of the tile; dh <= DP.  COPY: tiles travel to LDS by asynchronous copies (dh == DP, rows in the storage type), else through
@@ -284,27 +284,25 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int c = i * 256 + tid, r = c / CK, f = (c % CK) * 8;
-            const bool inside = f < a.dh;
+            const int fin = f < a.dh ? f : 0;   // (past the end of a row: something that is there, made zero below)
             int64_t kat, vat;
             if constexpr (SRC == KV_PACKED) {
                 const int64_t t = it.first + min(kt * KT + r, it.kv - 1);
-                kat = t * a.ldk + (int64_t)hk * a.dh + f;
-                vat = t * a.ldv + (int64_t)hk * a.dh + f;
+                kat = t * a.ldk + (int64_t)hk * a.dh + fin;
+                vat = t * a.ldv + (int64_t)hk * a.dh + fin;
             } else {
                 const int64_t cr = cache_row(kt, r, __shfl(pg, r));
                 if constexpr (E4M3) { ke[i] = a.Ks[cr]; ve[i] = a.Vs[cr]; }
-                kat = vat = cr * a.dh + f;
+                kat = vat = cr * a.dh + fin;
             }
             if constexpr (E4M3) {
-                const uint2 z = make_uint2(0, 0);
-                const uint2 kc = inside ? *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.K) + kat) : z;
-                const uint2 vc = inside ? *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.V) + vat) : z;
+                const uint2 kc = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.K) + kat);
+                const uint2 vc = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.V) + vat);
                 kr[i] = make_uint4(kc.x, kc.y, 0, 0);
                 vr[i] = make_uint4(vc.x, vc.y, 0, 0);
             } else {
-                const uint4 z = make_uint4(0, 0, 0, 0);
-                kr[i] = inside ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.K) + kat) : z;
-                vr[i] = inside ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.V) + vat) : z;
+                kr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.K) + kat);
+                vr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.V) + vat);
             }
         }
     };
@@ -314,6 +312,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
             const int c = i * 256 + tid, r = c / CK, ch = c % CK;
             uint4 k = kr[i], v = vr[i];
             if constexpr (E4M3) { k = expand8(make_uint2(k.x, k.y), ke[i]); v = expand8(make_uint2(v.x, v.y), ve[i]); }
+            if (ch * 8 >= a.dh) k = v = make_uint4(0, 0, 0, 0);
             sK[stage][r * CK + (ch ^ tile_swz<CK>(r))] = k;
             sV[stage][r * CK + (ch ^ column_swz<DP>(r))] = v;
         }
@@ -429,7 +428,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
         if (min(last, it.kv - 1) > lim_tile0) {   // some row does not see all keys
             bool bad = false;
 #pragma unroll
-            for (int i = 0; i < NL; ++i) bad = bad || any_not_finite(V[i * 256 + tid]);
+            for (int i = 0; i < NL; ++i) bad |= any_not_finite(V[i * 256 + tid]);
             spoilt = __syncthreads_or(bad) != 0;
             if (spoilt) break;
         }
@@ -490,7 +489,10 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
 // ---------------------------------------------------------------------------
 constexpr int ROWS_S = 32, KT_S = 32;
 
-template <int DP, int SRC>
+// FULL: dh == DP.  WHOLE: the rows of a tile follow each other (pages of KT_S positions at least): scalar bases.  Every load is unconditional (past the
+// end of a row or of the keys it reads something that is there, and zeros replace it where it is used): a branch around a load makes the
+// compiler wait for all loads before it, which took 200 us instead of the time below.
+template <int DP, int SRC, bool FULL, bool WHOLE>
 __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(ServeArgs a, ServePlan p, float c_log2e) {
     constexpr bool E4M3 = SRC == KV_PAGED_E4M3;
     constexpr int CK = DP / 8, NKS = DP / 16, NCT = DP / 32;
@@ -541,51 +543,73 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
     const int32_t* table = SRC == KV_PACKED ? nullptr : a.table + it.seq * a.max_pages;
     const int page_mask = (1 << a.page_shift) - 1;
     const int prow = (l32 & ~0xC) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);   // the key of this lane's row of the score product
-    const auto page_of = [&](int kt) {   // of key kt·KT_S + l32, -1 behind the last key
-        const int key = kt * KT_S + l32;
-        if (kt >= kt_end || key >= it.kv) return -1;
-        if constexpr (SRC == KV_PACKED) return 0;
-        else return table[key >> a.page_shift];
+    const auto page_of = [&](int kt) {   // of key kt·KT_S + prow, -1 behind the last key
+        const int key = kt * KT_S + prow;
+        if constexpr (SRC == KV_PACKED) return key < it.kv ? 0 : -1;
+        else {
+            const int page = table[min(key, it.kv - 1) >> a.page_shift];
+            return key < it.kv ? page : -1;
+        }
     };
-    const bool whole = SRC == KV_PACKED || a.page_shift >= 5;   // the rows of a tile follow each other
-    // element offset of key row r of a tile; any row for a key that is not there
+    // element offset of the row of tile row r (packed), or its row of the cache; any row for a key that is not there
     const auto row_at = [&](int kt, int r, int pg, int64_t ld) -> int64_t {
         if constexpr (SRC == KV_PACKED) return (int64_t)(it.first + min(kt * KT_S + r, it.kv - 1)) * ld + (int64_t)hk * a.dh;
-        const int pr = whole ? __builtin_amdgcn_readfirstlane(pg) : __shfl(pg, r);
-        const int page = pr >= 0 && pr < a.n_pages ? pr : 0;
-        return (((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * KT_S + r) & page_mask);   // row of the cache
+        const int page = (unsigned)pg < (unsigned)a.n_pages ? pg : 0;
+        return (((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * KT_S + r) & page_mask);
     };
-    const bool even = !E4M3 || a.dh % 16 == 0;
-    const auto piece = [&](const void* base, int64_t at, int f) {   // 16 bytes of a row, zeros past its end
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if constexpr (E4M3) {
-            const uint8_t* q = reinterpret_cast<const uint8_t*>(base) + at * a.dh + f;
-            if (even) { if (f < a.dh) v = *reinterpret_cast<const uint4*>(q); }
-            else {
-                if (f < a.dh) { const uint2 x = *reinterpret_cast<const uint2*>(q); v.x = x.x; v.y = x.y; }
-                if (f + 8 < a.dh) { const uint2 x = *reinterpret_cast<const uint2*>(q + 8); v.z = x.x; v.w = x.y; }
-            }
-        } else {
-            const bf16_t* q = reinterpret_cast<const bf16_t*>(base) + (SRC == KV_PACKED ? at : at * a.dh) + f;
-            if (f < a.dh) v = *reinterpret_cast<const uint4*>(q);
+    constexpr int ES = E4M3 ? 1 : 2;
+    const auto piece = [&](const void* base, int64_t at, int f) {   // 16 bytes of a row from feature f on (of some other where the row is shorter)
+        const uint8_t* q = reinterpret_cast<const uint8_t*>(base) + (SRC == KV_PACKED ? at : at * a.dh) * ES;
+        if constexpr (FULL || !E4M3) return *reinterpret_cast<const uint4*>(q + (FULL || f < a.dh ? f : 0) * ES);
+        else {
+            const uint2 x = *reinterpret_cast<const uint2*>(q + (f < a.dh ? f : 0)), y = *reinterpret_cast<const uint2*>(q + (f + 8 < a.dh ? f + 8 : 0));
+            return make_uint4(x.x, x.y, y.x, y.y);
+        }
+    };
+    // zeros for what lies past the end of a row
+    const auto cut = [&](uint4 v, int f) {
+        if constexpr (!FULL) {
+            if (f >= a.dh) v.x = v.y = 0;
+            if (f + (E4M3 ? 8 : 0) >= a.dh) v.z = v.w = 0;
         }
         return v;
     };
     uint4 kr[NK], vr[NV];
     int ke = 0, ve[E4M3 ? NV : 1];
+    const int k_at = prow, v_at = lane / LPR;   // rows of a tile that this lane loads: one of keys, every 64 / LPR-th of values
     const auto load_keys = [&](int kt, int pg) {
-        const int64_t at = row_at(kt, prow, pg, a.ldk);
-        if constexpr (E4M3) ke = a.Ks[at];
+        if constexpr (WHOLE) {
+            const int64_t r0 = row_at(kt, 0, __builtin_amdgcn_readfirstlane(pg), 0);
+            if constexpr (E4M3) ke = (a.Ks + r0)[(unsigned)k_at];
+            const uint8_t* q = reinterpret_cast<const uint8_t*>(a.K) + r0 * (DP * ES);
 #pragma unroll
-        for (int i = 0; i < NK; ++i) kr[i] = piece(a.K, at, 2 * EPL * i + EPL * lh);
+            for (int i = 0; i < NK; ++i) kr[i] = *reinterpret_cast<const uint4*>(q + (unsigned)(k_at * DP + 2 * EPL * i + EPL * lh) * ES);
+        } else {
+            const int64_t at = row_at(kt, k_at, pg, a.ldk);
+            if constexpr (E4M3) ke = a.Ks[at];
+#pragma unroll
+            for (int i = 0; i < NK; ++i) kr[i] = piece(a.K, at, 2 * EPL * i + EPL * lh);
+        }
     };
+    const auto perm = [](int r) { return (r & ~0xC) | ((r & 4) << 1) | ((r & 8) >> 1); };
     const auto load_values = [&](int kt, int pg) {
+        if constexpr (WHOLE) {
+            const int64_t r0 = row_at(kt, 0, __builtin_amdgcn_readfirstlane(pg), 0);
+            const uint8_t* q = reinterpret_cast<const uint8_t*>(a.V) + r0 * (DP * ES);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int r = i * (64 / LPR) + lane / LPR;
-            const int64_t at = row_at(kt, r, pg, a.ldv);
-            if constexpr (E4M3) ve[i] = a.Vs[at];
-            vr[i] = piece(a.V, at, EPL * (lane % LPR));
+            for (int i = 0; i < NV; ++i) {
+                const int r = i * (64 / LPR) + v_at;
+                if constexpr (E4M3) ve[i] = (a.Vs + r0)[(unsigned)r];
+                vr[i] = *reinterpret_cast<const uint4*>(q + (unsigned)(r * DP + EPL * (lane % LPR)) * ES);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int r = i * (64 / LPR) + v_at;
+                const int64_t at = row_at(kt, r, SRC == KV_PACKED ? 0 : __shfl(pg, perm(r)), a.ldv);
+                if constexpr (E4M3) ve[i] = a.Vs[at];
+                vr[i] = piece(a.V, at, EPL * (lane % LPR));
+            }
         }
     };
     uint4* V = sV[wave];
@@ -596,9 +620,14 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
     bool spoilt = false;
 
     int kt = kt_begin + wave;
-    int pg0 = page_of(kt), pg1 = page_of(kt + 4);
+    int pg0 = -1, pg1 = -1;
+    if (kt < kt_end) {
+        pg0 = page_of(kt);
+        pg1 = page_of(kt + 4);
+    }
     if (kt < kt_end) { load_keys(kt, pg0); load_values(kt, pg0); }
     for (; kt < kt_end; kt += 4) {
+        // bit i: the key of row i of the score product is there
         const unsigned alive = (unsigned)__builtin_amdgcn_ballot_w64(pg0 >= 0 && (SRC == KV_PACKED || pg0 < a.n_pages));
         const int pg2 = page_of(kt + 8);
         f32x16 s;
@@ -606,12 +635,13 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
         for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
+            const uint4 kc = cut(kr[i], 2 * EPL * i + EPL * lh);
             if constexpr (E4M3) {
-                const bf16x8 k0 = u4_as_bf16x8(expand8(make_uint2(kr[i].x, kr[i].y), ke)), k1 = u4_as_bf16x8(expand8(make_uint2(kr[i].z, kr[i].w), ke));
+                const bf16x8 k0 = u4_as_bf16x8(expand8(make_uint2(kc.x, kc.y), ke)), k1 = u4_as_bf16x8(expand8(make_uint2(kc.z, kc.w), ke));
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qf[2 * i], s, 0, 0, 0);
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qf[2 * i + 1], s, 0, 0, 0);
             } else {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u4_as_bf16x8(kr[i]), qf[i], s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u4_as_bf16x8(kc), qf[i], s, 0, 0, 0);
             }
         }
         if (kt + 4 < kt_end) load_keys(kt + 4, pg1);
@@ -619,16 +649,17 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int r = i * (64 / LPR) + lane / LPR, f = lane % LPR;
-            const bool there = (alive >> r) & 1;   // a weight of zero does not take NaN away: values of keys that are not there are zeros
+            const bool there = (alive >> perm(r)) & 1;   // a weight of zero does not take NaN away: values of keys that are not there are zeros
+            const uint4 vc = cut(vr[i], EPL * f);
             if constexpr (E4M3) {
-                uint4 lo = expand8(make_uint2(vr[i].x, vr[i].y), ve[i]), hi = expand8(make_uint2(vr[i].z, vr[i].w), ve[i]);
+                uint4 lo = expand8(make_uint2(vc.x, vc.y), ve[i]), hi = expand8(make_uint2(vc.z, vc.w), ve[i]);
                 if (!there) lo = hi = make_uint4(0, 0, 0, 0);
-                if (partial) bad = bad || any_not_finite(lo) || any_not_finite(hi);
+                if (partial) bad |= any_not_finite(lo) | any_not_finite(hi);
                 V[r * CK + ((2 * f) ^ column_swz<DP>(r))] = lo;
                 V[r * CK + ((2 * f + 1) ^ column_swz<DP>(r))] = hi;
             } else {
-                const uint4 v = there ? vr[i] : make_uint4(0, 0, 0, 0);
-                if (partial) bad = bad || any_not_finite(v);
+                const uint4 v = there ? vc : make_uint4(0, 0, 0, 0);
+                if (partial) bad |= any_not_finite(v);
                 V[r * CK + (f ^ column_swz<DP>(r))] = v;
             }
         }
@@ -638,7 +669,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int key = 16 * (v >> 3) + 8 * lh + (v & 7);
-                if (kt * KT_S + key > lim || !((alive >> key) & 1)) s[v] = -INFINITY;
+                if (kt * KT_S + key > lim || !((alive >> perm(key)) & 1)) s[v] = -INFINITY;
             }
         }
         float mloc = -INFINITY;
@@ -812,9 +843,19 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool f
     const dim3 grid((unsigned)blocks);
     const bool copy = a.dh == DP;
     if (few) {
-        if (src == KV_PACKED) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED>), grid, dim3(256), 0, st, a, p, c);
-        else if (src == KV_PAGED) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED>), grid, dim3(256), 0, st, a, p, c);
-        else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a, p, c);
+        const bool whole = a.page_shift >= 5;
+        if (src == KV_PACKED) {
+            if (copy) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED, true, false>), grid, dim3(256), 0, st, a, p, c);
+            else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED, false, false>), grid, dim3(256), 0, st, a, p, c);
+        } else if (src == KV_PAGED) {
+            if (copy && whole) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else if (copy) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, true, false>), grid, dim3(256), 0, st, a, p, c);
+            else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, false, false>), grid, dim3(256), 0, st, a, p, c);
+        } else {
+            if (copy && whole) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else if (copy) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, true, false>), grid, dim3(256), 0, st, a, p, c);
+            else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, false, false>), grid, dim3(256), 0, st, a, p, c);
+        }
     } else if (src == KV_PACKED) {
         if (copy) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, true>), grid, dim3(256), 0, st, a, p, c);
         else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, false>), grid, dim3(256), 0, st, a, p, c);
