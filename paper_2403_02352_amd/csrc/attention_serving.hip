@@ -2,6 +2,7 @@
 #include "serving.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace atp {
 namespace {
@@ -154,22 +155,34 @@ __device__ __forceinline__ uint4 expand8(uint2 c, int byte) {
     return o.u;
 }
 
-__device__ __forceinline__ bool any_not_finite(const uint4& u) {
-    const auto word = [](uint32_t x) { return ((x & 0x7f80u) == 0x7f80u) | ((x & 0x7f800000u) == 0x7f800000u); };
-    return word(u.x) | word(u.y) | word(u.z) | word(u.w);
-}
+// whether any of the bf16 values taken so far is infinite or NaN
+struct NotFinite {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
+    __device__ __forceinline__ void take(uint32_t w) {
+        union { uint32_t u; u16x2 h; } c;
+        c.u = w & 0x7fff7fffu;
+        top = __builtin_elementwise_max(top, c.h);
+    }
+    __device__ __forceinline__ void take(const uint4& u) { take(u.x); take(u.y); take(u.z); take(u.w); }
+    __device__ __forceinline__ bool any() const { return (top[0] >= 0x7f80) | (top[1] >= 0x7f80); }
+};
 
-// DP: head width of the tile; dh <= DP.  COPY: tiles travel to LDS by asynchronous copies (dh == DP, rows in the storage type), else through
-// registers, where codes become bf16 and missing columns zeros.
-template <int DP, int SRC, bool COPY>
+// DP: head width of the tile, dh <= DP.  FULL: dh == DP.  WHOLE: the rows of a tile follow each other (packed keys, pages of KT positions at
+// least), so tiles have scalar bases and lane offsets that stay the same.  Full rows in the storage type travel to LDS by asynchronous copies,
+// others through registers, where codes become bf16 and columns past the end of a row zeros.
+template <int DP, int SRC, bool FULL, bool WHOLE>
 __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(ServeArgs a, ServePlan p, float c_log2e) {
     constexpr int CK = DP / 8;            // 16-byte chunks of a row
     constexpr int NKS = DP / 16, NCT = DP / 32, NT = KT / 32;
+    constexpr bool E4M3 = SRC == KV_PAGED_E4M3, PACKED = SRC == KV_PACKED, COPY = FULL && !E4M3;
     constexpr int KRPI = 64 / CK;         // rows of a copy instruction
-    constexpr int NKI = KT / KRPI / 4;    // copy instructions of a wave for a tile of keys
-    constexpr bool E4M3 = SRC == KV_PAGED_E4M3;
-    __shared__ __align__(16) uint4 sK[2][KT * CK];
-    __shared__ __align__(16) uint4 sV[2][KT * CK];
+    constexpr int NL = KT * CK / 256;     // 16-byte chunks of a tile of keys that a thread moves
+    __shared__ __align__(16) uint4 sK0[KT * CK];
+    __shared__ __align__(16) uint4 sK1[KT * CK];
+    __shared__ __align__(16) uint4 sV0[KT * CK];
+    __shared__ __align__(16) uint4 sV1[KT * CK];
+    __shared__ int sSpoilt;
 
     const int hk = blockIdx.x % a.kv_heads;   // consecutive workgroups go to the 8 XCDs in turn: a key head's items share an L2
     ServeItem it;
@@ -177,17 +190,15 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, lh = lane >> 5;
     const unsigned group = a.heads / a.kv_heads;
+    if (tid == 0) sSpoilt = 0;
 
-    // last key that a row sees (-1: none); rows of a tile see more and more
+    // last key that a row sees (negative: none); rows of a tile see more and more
     const auto last_key = [&](int row) { return a.causal ? min(it.p0 + (int)((unsigned)row / group), it.kv - 1) : it.kv - 1; };
-    const int row = it.row0 + wave * 32 + l32;
+    const int wrow0 = it.row0 + wave * 32, row = wrow0 + l32;
     const bool live_row = row < it.rows;
-    const int token = it.first + (int)((unsigned)row / group), head = hk * (int)group + (int)((unsigned)row % group);
     const int lim = live_row ? last_key(row) : -1;
     const int lim_tile0 = last_key(it.row0), lim_tile1 = last_key(min(it.row0 + ROWS, it.rows) - 1);
-    const int wrow0 = it.row0 + wave * 32;
-    const bool live_wave = wrow0 < it.rows;
-    const int lim_wave0 = live_wave ? last_key(wrow0) : -1, lim_wave1 = live_wave ? last_key(min(wrow0 + 32, it.rows) - 1) : -1;
+    const int lim_wave0 = wrow0 < it.rows ? last_key(wrow0) : -1, lim_wave1 = wrow0 < it.rows ? last_key(min(wrow0 + 32, it.rows) - 1) : -1;
 
     // key tiles of this item
     const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
@@ -195,12 +206,14 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
 
     bf16x8 qf[NKS];
     {
-        const bf16_t* Qp = reinterpret_cast<const bf16_t*>(a.Q) + (int64_t)token * a.ldq + (int64_t)head * a.dh;
+        const int qrow = min(row, it.rows - 1);   // rows past the end: any row, stored by nobody
+        const int64_t token = it.first + (int)((unsigned)qrow / group), head = hk * (int)group + (int)((unsigned)qrow % group);
+        const bf16_t* Qp = reinterpret_cast<const bf16_t*>(a.Q) + token * a.ldq + head * a.dh;
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) {
             const int c = ks * 16 + lh * 8;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (live_row && (COPY || c < a.dh)) v = *reinterpret_cast<const uint4*>(Qp + c);
+            uint4 v = *reinterpret_cast<const uint4*>(Qp + (FULL || c < a.dh ? c : 0));
+            if (!FULL && c >= a.dh) v = make_uint4(0, 0, 0, 0);
             qf[ks] = u4_as_bf16x8(v);
         }
     }
@@ -212,109 +225,90 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     float m_run = -INFINITY, l_run = 0.f;
 
     // ---- where keys come from -------------------------------------------------------
-    const int32_t* table = SRC == KV_PACKED ? nullptr : a.table + it.seq * a.max_pages;
+    const int32_t* table = PACKED ? nullptr : a.table + it.seq * a.max_pages;
     const int page_mask = (1 << a.page_shift) - 1;
     // page of key kt·KT + lane, -1 behind the last key
     const auto page_of = [&](int kt) {
-        const int key = kt * KT + lane;
-        if constexpr (SRC == KV_PACKED) return key < it.kv ? 0 : -1;
-        else return key < it.kv ? table[key >> a.page_shift] : -1;
+        const int key = kt * KT + lane, page = table[min(key, it.kv - 1) >> a.page_shift];
+        return key < it.kv ? page : -1;
     };
-    // first row of the cache that key `kt·KT + r` (its page `pg`) lies in; any row there is for a key that is not
-    const auto cache_row = [&](int kt, int r, int pg) {
-        const int page = pg >= 0 && pg < a.n_pages ? pg : 0;
-        return ((((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * KT + r) & page_mask));
+    // row of the cache of tile row r, whose page is pg; any row for a key that is not there
+    const auto cache_row = [&](int kt, int r, int pg) -> int64_t {
+        const int page = (unsigned)pg < (unsigned)a.n_pages ? pg : 0;
+        return (((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * KT + r) & page_mask);
     };
+    // keys of a tile that are there
+    const auto alive_of = [&](int kt, int pg) -> unsigned long long {
+        if constexpr (PACKED) {
+            const int n = it.kv - kt * KT;
+            return n >= KT ? ~0ull : (1ull << n) - 1;
+        } else return __builtin_amdgcn_ballot_w64((unsigned)pg < (unsigned)a.n_pages);
+    };
+    constexpr int ES = E4M3 ? 1 : 2;
+    const unsigned kb = (PACKED ? (unsigned)a.ldk : (unsigned)a.dh) * ES, vb = (PACKED ? (unsigned)a.ldv : (unsigned)a.dh) * ES;   // bytes between rows
+    const uint8_t* Kh = reinterpret_cast<const uint8_t*>(a.K) + (PACKED ? ((int64_t)it.first * a.ldk + (int64_t)hk * a.dh) * ES : 0);
+    const uint8_t* Vh = reinterpret_cast<const uint8_t*>(a.V) + (PACKED ? ((int64_t)it.first * a.ldv + (int64_t)hk * a.dh) * ES : 0);
+    // rows and chunks of a tile that this thread moves: row(i) = i·RSTEP + row0, the same chunk each time
+    constexpr int RSTEP = 256 / CK;
+    const int m_row = COPY ? wave * KRPI + lane / CK : tid / CK, m_ch = COPY ? lane % CK : tid % CK;
+    const unsigned m_f = FULL || m_ch * 8 < a.dh ? (unsigned)m_ch * 8u * ES : 0u;   // its byte offset in a row that is read (past the end: the first)
     const unsigned wave_s = (unsigned)wave * 1024u;
-    const unsigned lK = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)&sK[0][0]) + wave_s;
-    const unsigned lV = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)&sV[0][0]) + wave_s;
-    constexpr unsigned STAGE = KT * CK * 16;
-    // A tile whose rows follow each other (packed, or within one page) is copied from a scalar base with lane offsets that stay the same;
-    // pages shorter than a tile give every lane an address of its own.
-    const bool whole = SRC == KV_PACKED || a.page_shift >= 6;
-    const unsigned kb = SRC == KV_PACKED ? (unsigned)a.ldk * 2u : DP * 2u, vb = SRC == KV_PACKED ? (unsigned)a.ldv * 2u : DP * 2u;
-    unsigned k_ofs[NKI], v_ofs[NKI];
+    const auto lds = [&](const uint4* x) { return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)x) + wave_s; };
+    const unsigned lK0 = lds(sK0), lK1 = lds(sK1), lV0 = lds(sV0), lV1 = lds(sV1);
+    const auto copy_tile = [&](int kt, int pg, bool odd) {
+        const unsigned lk = odd ? lK1 : lK0, lv = odd ? lV1 : lV0;
+        if constexpr (WHOLE) {
+            int64_t r0 = PACKED ? (int64_t)(kt * KT) : cache_row(kt, 0, __builtin_amdgcn_readfirstlane(pg));
+            const uint8_t *K = Kh + r0 * kb, *V = Vh + r0 * vb;
+            const int last = PACKED ? it.kv - 1 - kt * KT : KT - 1;   // rows past the end: the last one, they weigh nothing
 #pragma unroll
-    for (int i = 0; i < NKI; ++i) {
-        const int r = (i * 4 + wave) * KRPI + lane / CK;
-        k_ofs[i] = (unsigned)r * kb + (unsigned)((lane % CK) ^ tile_swz<CK>(r)) * 16u;
-        v_ofs[i] = (unsigned)r * vb + (unsigned)((lane % CK) ^ column_swz<DP>(r)) * 16u;
-    }
-    const bf16_t* Kh = reinterpret_cast<const bf16_t*>(a.K) + (SRC == KV_PACKED ? (int64_t)it.first * a.ldk + (int64_t)hk * DP : 0);
-    const bf16_t* Vh = reinterpret_cast<const bf16_t*>(a.V) + (SRC == KV_PACKED ? (int64_t)it.first * a.ldv + (int64_t)hk * DP : 0);
-    const auto copy_tile = [&](int kt, int pg, int stage) {
-        const unsigned lk = lK + (unsigned)stage * STAGE, lv = lV + (unsigned)stage * STAGE;
-        if (whole && (SRC != KV_PACKED || kt * KT + KT <= it.kv)) {
-            const bf16_t *K = Kh, *V = Vh;
-            if constexpr (SRC == KV_PACKED) {
-                K += (int64_t)(kt * KT) * a.ldk;
-                V += (int64_t)(kt * KT) * a.ldv;
-            } else {
-                const int64_t r = cache_row(kt, 0, __builtin_amdgcn_readfirstlane(pg)) * DP;
-                K += r;
-                V += r;
+            for (int i = 0; i < NL; ++i) {
+                const int r = i * RSTEP + m_row;
+                const unsigned rr = PACKED ? (unsigned)min(r, last) : (unsigned)r;
+                copy16_untracked(K, rr * kb + (unsigned)((m_ch ^ tile_swz<CK>(r)) * 16), lk + (unsigned)i * 4096u);
+                copy16_untracked(V, rr * vb + (unsigned)((m_ch ^ column_swz<DP>(r)) * 16), lv + (unsigned)i * 4096u);
             }
+        } else {
 #pragma unroll
-            for (int i = 0; i < NKI; ++i) {
-                copy16_untracked(K, k_ofs[i], lk + (unsigned)i * 4096u);
-                copy16_untracked(V, v_ofs[i], lv + (unsigned)i * 4096u);
+            for (int i = 0; i < NL; ++i) {
+                const int r = i * RSTEP + m_row;
+                const int64_t at = cache_row(kt, r, __shfl(pg, r));
+                copy16_far(Kh + at * kb + (m_ch ^ tile_swz<CK>(r)) * 16, lk + (unsigned)i * 4096u);
+                copy16_far(Vh + at * vb + (m_ch ^ column_swz<DP>(r)) * 16, lv + (unsigned)i * 4096u);
             }
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < NKI; ++i) {
-            const int r = (i * 4 + wave) * KRPI + lane / CK;
-            const unsigned kc = k_ofs[i] - (unsigned)r * kb, vc = v_ofs[i] - (unsigned)r * vb;
-            int64_t kat, vat;
-            if constexpr (SRC == KV_PACKED) {
-                const int64_t t = min(kt * KT + r, it.kv - 1);   // rows past the end: any row, they weigh nothing
-                kat = t * a.ldk;
-                vat = t * a.ldv;
-            } else {
-                kat = vat = cache_row(kt, r, __shfl(pg, r)) * DP;
-            }
-            copy16_far(reinterpret_cast<const uint8_t*>(Kh + kat) + kc, lk + (unsigned)i * 4096u);
-            copy16_far(reinterpret_cast<const uint8_t*>(Vh + vat) + vc, lv + (unsigned)i * 4096u);
         }
     };
-    constexpr int NL = KT * CK / 256;   // chunks of a thread
-    uint4 kr[COPY ? 1 : NL], vr[COPY ? 1 : NL];
+    typedef typename std::conditional<E4M3, uint2, uint4>::type Piece;
+    Piece kr[COPY ? 1 : NL], vr[COPY ? 1 : NL];
     int ke[E4M3 ? NL : 1], ve[E4M3 ? NL : 1];
     const auto load_tile = [&](int kt, int pg) {
+        const int64_t r0 = !WHOLE ? 0 : PACKED ? (int64_t)(kt * KT) : cache_row(kt, 0, __builtin_amdgcn_readfirstlane(pg));
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int c = i * 256 + tid, r = c / CK, f = (c % CK) * 8;
-            const int fin = f < a.dh ? f : 0;   // (past the end of a row: something that is there, made zero below)
-            int64_t kat, vat;
-            if constexpr (SRC == KV_PACKED) {
-                const int64_t t = it.first + min(kt * KT + r, it.kv - 1);
-                kat = t * a.ldk + (int64_t)hk * a.dh + fin;
-                vat = t * a.ldv + (int64_t)hk * a.dh + fin;
+            const int r = i * RSTEP + m_row;
+            if constexpr (WHOLE) {
+                const unsigned rr = PACKED ? (unsigned)min(r, it.kv - 1 - kt * KT) : (unsigned)r;
+                if constexpr (E4M3) { ke[i] = (a.Ks + r0)[rr]; ve[i] = (a.Vs + r0)[rr]; }
+                kr[i] = *reinterpret_cast<const Piece*>(Kh + r0 * kb + (rr * kb + m_f));
+                vr[i] = *reinterpret_cast<const Piece*>(Vh + r0 * vb + (rr * vb + m_f));
             } else {
-                const int64_t cr = cache_row(kt, r, __shfl(pg, r));
-                if constexpr (E4M3) { ke[i] = a.Ks[cr]; ve[i] = a.Vs[cr]; }
-                kat = vat = cr * a.dh + fin;
-            }
-            if constexpr (E4M3) {
-                const uint2 kc = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.K) + kat);
-                const uint2 vc = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(a.V) + vat);
-                kr[i] = make_uint4(kc.x, kc.y, 0, 0);
-                vr[i] = make_uint4(vc.x, vc.y, 0, 0);
-            } else {
-                kr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.K) + kat);
-                vr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.V) + vat);
+                const int64_t at = cache_row(kt, r, __shfl(pg, r));
+                if constexpr (E4M3) { ke[i] = a.Ks[at]; ve[i] = a.Vs[at]; }
+                kr[i] = *reinterpret_cast<const Piece*>(Kh + at * kb + m_f);
+                vr[i] = *reinterpret_cast<const Piece*>(Vh + at * vb + m_f);
             }
         }
     };
-    const auto store_tile = [&](int stage) {
+    const auto store_tile = [&](uint4* K, uint4* V) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int c = i * 256 + tid, r = c / CK, ch = c % CK;
-            uint4 k = kr[i], v = vr[i];
-            if constexpr (E4M3) { k = expand8(make_uint2(k.x, k.y), ke[i]); v = expand8(make_uint2(v.x, v.y), ve[i]); }
-            if (ch * 8 >= a.dh) k = v = make_uint4(0, 0, 0, 0);
-            sK[stage][r * CK + (ch ^ tile_swz<CK>(r))] = k;
-            sV[stage][r * CK + (ch ^ column_swz<DP>(r))] = v;
+            const int r = i * RSTEP + m_row;
+            uint4 k, v;
+            if constexpr (E4M3) { k = expand8(kr[i], ke[i]); v = expand8(vr[i], ve[i]); }
+            else { k = kr[i]; v = vr[i]; }
+            if (!FULL && m_ch * 8 >= a.dh) k = v = make_uint4(0, 0, 0, 0);
+            K[r * CK + (m_ch ^ tile_swz<CK>(r))] = k;
+            V[r * CK + (m_ch ^ column_swz<DP>(r))] = v;
         }
     };
 
@@ -325,8 +319,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
 #pragma unroll
     for (int i = 0; i < NCT; ++i) v_col[i] = column_frag_offset<DP>(lane, 32 * i);
 
-    // alive: keys of the tile that are there; hidden: some row of this wave does not see all of them
-    const auto compute = [&](int kt, const uint4* K, const uint4* V, unsigned long long alive, bool hidden) {
+    const auto compute = [&](int kt, const uint4* K, const uint4* V, unsigned long long alive) {
         f32x16 s[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -338,14 +331,17 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
                 s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
             }
         }
-        if (hidden) {
+        if (kt * KT + KT - 1 > lim_wave0 || alive != ~0ull) {   // some row of this wave does not see all keys
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t) {
+                const unsigned there = (unsigned)(alive >> (32 * t)) >> (8 * lh);
+                const int upto = lim - (kt * KT + 32 * t + 8 * lh);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const int key = 32 * t + 16 * (v >> 3) + 8 * lh + (v & 7);
-                    if (kt * KT + key > lim || !((alive >> key) & 1)) s[t][v] = -INFINITY;
+                    const int key = 16 * (v >> 3) + (v & 7);   // past the lane half's first
+                    s[t][v] = key <= upto && ((there >> key) & 1) ? s[t][v] : -INFINITY;
                 }
+            }
         }
         float mloc = -INFINITY;
 #pragma unroll
@@ -394,49 +390,51 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
             }
     };
 
-    int pg = -1, pg_next = -1;
-    bool spoilt = false;   // the values hold something not finite where some row does not see all of them
-    if (kt_begin < kt_end) {
-        pg = page_of(kt_begin);
-        if constexpr (COPY) copy_tile(kt_begin, pg, 0);
-        else load_tile(kt_begin, pg);
-    }
-    for (int kt = kt_begin; kt < kt_end; ++kt) {
-        const int stage = (kt - kt_begin) & 1;
-        const unsigned long long alive = __builtin_amdgcn_ballot_w64(pg >= 0 && (SRC == KV_PACKED || pg < a.n_pages));
-        if (kt + 1 < kt_end) pg_next = page_of(kt + 1);
+    int pg0 = 0, pg1 = 0;   // pages of this tile's keys and the next one's
+    const auto step = [&](int kt, uint4* K, uint4* V, bool odd) {
+        int pg2 = 0;
         if constexpr (COPY) {
             __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's copies have landed (the compiler does not count them)
             __syncthreads();
-            if (kt + 1 < kt_end) copy_tile(kt + 1, pg_next, stage ^ 1);
+            if constexpr (!PACKED) pg2 = page_of(kt + 2);
+            if (kt + 1 < kt_end) copy_tile(kt + 1, pg1, !odd);
         } else {
-            store_tile(stage);
+            store_tile(K, V);
             __syncthreads();
-            if (kt + 1 < kt_end) load_tile(kt + 1, pg_next);
+            if constexpr (!PACKED) pg2 = page_of(kt + 2);
+            if (kt + 1 < kt_end) load_tile(kt + 1, pg1);
         }
-        uint4 *K = sK[stage], *V = sV[stage];
+        const unsigned long long alive = alive_of(kt, pg0);
         // values of keys that are not there become zeros: their weight is zero, but zero times NaN is not
         if (alive != ~0ull) {
-#pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                const int c = i * 256 + tid;
+            for (int c = tid; c < KT * CK; c += 256)
                 if (!((alive >> (c / CK)) & 1)) V[c] = make_uint4(0u, 0u, 0u, 0u);
-            }
             __syncthreads();
         }
-        const int last = kt * KT + KT - 1;
-        if (min(last, it.kv - 1) > lim_tile0) {   // some row does not see all keys
-            bool bad = false;
+        if (min(kt * KT + KT, it.kv) - 1 > lim_tile0) {   // some row does not see all keys: are their values finite?
+            NotFinite n;
 #pragma unroll
-            for (int i = 0; i < NL; ++i) bad |= any_not_finite(V[i * 256 + tid]);
-            spoilt = __syncthreads_or(bad) != 0;
-            if (spoilt) break;
+            for (int i = 0; i < NL; ++i) n.take(V[i * 256 + tid]);
+            if (n.any()) sSpoilt = 1;
         }
-        if (kt * KT <= lim_wave1) compute(kt, K, V, alive, last > lim_wave0 || alive != ~0ull);
-        pg = pg_next;
+        if (kt * KT <= lim_wave1) compute(kt, K, V, alive);
+        pg0 = pg1;
+        pg1 = pg2;
+    };
+    if (kt_begin < kt_end) {
+        if constexpr (!PACKED) {
+            pg0 = page_of(kt_begin);
+            pg1 = page_of(kt_begin + 1);
+        }
+        if constexpr (COPY) copy_tile(kt_begin, pg0, false);
+        else load_tile(kt_begin, pg0);
     }
-    if (spoilt) {
-        if constexpr (COPY) __builtin_amdgcn_s_waitcnt(0x0F70);   // no copy is left in flight
+    for (int kt = kt_begin; kt < kt_end; kt += 2) {
+        step(kt, sK0, sV0, false);
+        if (kt + 1 < kt_end) step(kt + 1, sK1, sV1, true);
+    }
+    __syncthreads();
+    if (sSpoilt) {
         attend_item_by_rows<bf16_t, SRC, ROWS>(a, p, it, hk, kt_begin * KT, kt_end * KT, DP);
         return;
     }
@@ -455,9 +453,8 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
         return;
     }
     const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
-    __syncthreads();
     // the output turns in LDS, one stage array a wave, so that a row leaves as 16-byte pieces
-    bf16_t* ob = reinterpret_cast<bf16_t*>(wave < 2 ? sK[wave] : sV[wave - 2]);
+    bf16_t* ob = reinterpret_cast<bf16_t*>(wave == 0 ? sK0 : wave == 1 ? sK1 : wave == 2 ? sV0 : sV1);
 #pragma unroll
     for (int i = 0; i < NCT; ++i)
 #pragma unroll
@@ -645,7 +642,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
             }
         }
         if (kt + 4 < kt_end) load_keys(kt + 4, pg1);
-        bool bad = false;
+        NotFinite seen;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int r = i * (64 / LPR) + lane / LPR, f = lane % LPR;
@@ -654,17 +651,17 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
             if constexpr (E4M3) {
                 uint4 lo = expand8(make_uint2(vc.x, vc.y), ve[i]), hi = expand8(make_uint2(vc.z, vc.w), ve[i]);
                 if (!there) lo = hi = make_uint4(0, 0, 0, 0);
-                if (partial) bad |= any_not_finite(lo) | any_not_finite(hi);
+                if (partial) { seen.take(lo); seen.take(hi); }
                 V[r * CK + ((2 * f) ^ column_swz<DP>(r))] = lo;
                 V[r * CK + ((2 * f + 1) ^ column_swz<DP>(r))] = hi;
             } else {
                 const uint4 v = there ? vc : make_uint4(0, 0, 0, 0);
-                if (partial) bad |= any_not_finite(v);
+                if (partial) seen.take(v);
                 V[r * CK + (f ^ column_swz<DP>(r))] = v;
             }
         }
         if (kt + 4 < kt_end) load_values(kt + 4, pg1);
-        if (min(kt * KT_S + KT_S, it.kv) - 1 > lim0 && __builtin_amdgcn_ballot_w64(bad) != 0) spoilt = true;
+        if (min(kt * KT_S + KT_S, it.kv) - 1 > lim0 && seen.any()) spoilt = true;
         if (kt * KT_S + KT_S - 1 > lim0 || alive != ~0u) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
@@ -709,7 +706,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
         pg0 = pg1;
         pg1 = pg2;
     }
-    if (spoilt && lane == 0) sSpoilt = 1;
+    if (spoilt) sSpoilt = 1;
     __syncthreads();
     if (sSpoilt) {
         attend_item_by_rows<bf16_t, SRC, ROWS_S>(a, p, it, hk, kt_begin * KT_S, kt_end * KT_S, DP);
@@ -841,29 +838,34 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool f
     const int64_t blocks = (int64_t)p.items * a.kv_heads;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
-    const bool copy = a.dh == DP;
+    const bool full = a.dh == DP;
     if (few) {
         const bool whole = a.page_shift >= 5;
         if (src == KV_PACKED) {
-            if (copy) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED, true, false>), grid, dim3(256), 0, st, a, p, c);
+            if (full) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED, true, false>), grid, dim3(256), 0, st, a, p, c);
             else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PACKED, false, false>), grid, dim3(256), 0, st, a, p, c);
         } else if (src == KV_PAGED) {
-            if (copy && whole) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, true, true>), grid, dim3(256), 0, st, a, p, c);
-            else if (copy) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, true, false>), grid, dim3(256), 0, st, a, p, c);
+            if (full && whole) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else if (full) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, true, false>), grid, dim3(256), 0, st, a, p, c);
             else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED, false, false>), grid, dim3(256), 0, st, a, p, c);
         } else {
-            if (copy && whole) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, true, true>), grid, dim3(256), 0, st, a, p, c);
-            else if (copy) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, true, false>), grid, dim3(256), 0, st, a, p, c);
+            if (full && whole) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else if (full) hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, true, false>), grid, dim3(256), 0, st, a, p, c);
             else hipLaunchKernelGGL((attn_few_rows_kernel<DP, KV_PAGED_E4M3, false, false>), grid, dim3(256), 0, st, a, p, c);
         }
-    } else if (src == KV_PACKED) {
-        if (copy) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, true>), grid, dim3(256), 0, st, a, p, c);
-        else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, false>), grid, dim3(256), 0, st, a, p, c);
-    } else if (src == KV_PAGED) {
-        if (copy) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, true>), grid, dim3(256), 0, st, a, p, c);
-        else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, false>), grid, dim3(256), 0, st, a, p, c);
     } else {
-        hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED_E4M3, false>), grid, dim3(256), 0, st, a, p, c);
+        const bool whole = a.page_shift >= 6;
+        if (src == KV_PACKED) {
+            if (full) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PACKED, false, true>), grid, dim3(256), 0, st, a, p, c);
+        } else if (src == KV_PAGED) {
+            if (full && whole) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else if (full) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, true, false>), grid, dim3(256), 0, st, a, p, c);
+            else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED, false, false>), grid, dim3(256), 0, st, a, p, c);
+        } else {
+            if (full && whole) hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED_E4M3, true, true>), grid, dim3(256), 0, st, a, p, c);
+            else hipLaunchKernelGGL((attn_tiles_kernel<DP, KV_PAGED_E4M3, false, false>), grid, dim3(256), 0, st, a, p, c);
+        }
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part_rows) return e;
