@@ -104,33 +104,6 @@ __device__ __forceinline__ void attend_item_by_rows(const ServeArgs& a, const Se
     }
 }
 
-template <typename T, int SRC>
-__global__ void __launch_bounds__(256) attn_rows_kernel(ServeArgs a) {
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int token = __builtin_amdgcn_readfirstlane((int)(w / a.heads)), h = __builtin_amdgcn_readfirstlane((int)(w % a.heads));
-    if (token >= a.tokens) return;
-    const int s = sequence_of(a, token);
-    if (s < 0) return;
-    int first, n;
-    sequence_rows(a, s, first, n);
-    const int held = SRC == KV_PACKED ? n : max(a.length[s], 0);
-    const int pos = held - n + (token - first);
-    int keys = SRC == KV_PACKED ? n : min(held, a.max_kv);
-    if (a.causal) keys = min(keys, pos + 1);
-    const RowSum r = attend_row<T, SRC>(a, s, first, h / (a.heads / a.kv_heads), reinterpret_cast<const T*>(a.Q) + (int64_t)token * a.ldq + (int64_t)h * a.dh, 0, keys);
-    store_row(reinterpret_cast<T*>(a.O) + (int64_t)token * a.ldo + (int64_t)h * a.dh, r, a.dh);
-}
-
-template <typename T>
-hipError_t launch_rows(hipStream_t st, const ServeArgs& a, KvSource src) {
-    const int64_t blocks = ((int64_t)a.tokens * a.heads + 3) / 4;
-    const dim3 grid((unsigned)blocks);
-    if (src == KV_PACKED) hipLaunchKernelGGL((attn_rows_kernel<T, KV_PACKED>), grid, dim3(256), 0, st, a);
-    else if (src == KV_PAGED) hipLaunchKernelGGL((attn_rows_kernel<T, KV_PAGED>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((attn_rows_kernel<T, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a);
-    return hipGetLastError();
-}
-
 // ---------------------------------------------------------------------------
 // bf16: tiles of 128 rows and 64 keys on the matrix cores, scores transposed (a row to a lane) as in the attention over principal keys.
 // ---------------------------------------------------------------------------
@@ -763,6 +736,247 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
         }
 }
 
+// ---------------------------------------------------------------------------
+// fp32: tiles of 32 rows a wave and 32 keys on v_mfma_f32_32x32x2f32 (products and sums in fp32), scores transposed, a row to a lane.  Accumulator
+// register v of lane half lh belongs to key 8·(v/4) + 4·lh + v%4, so it is at once the operand of a step of Oᵀ += Vᵀ·Pᵀ over the two keys of
+// its halves, and values are read as they lie.  KS = 1: four waves of 32 rows share the keys; KS = 4: one block of 32 rows, its key tiles dealt to
+// four waves that meet at the end (few rows).  Bound by the fp32 matrix cores (256 flop per clock and compute unit).
+// ---------------------------------------------------------------------------
+template <int DP, int KS, int SRC>
+__global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, ServePlan p) {
+    constexpr bool E4M3 = SRC == KV_PAGED_E4M3, PACKED = SRC == KV_PACKED;
+    constexpr int ROWS_ = 128 / KS, TK = 32 * KS;   // rows of an item, keys of a stage
+    constexpr int PK = DP + 4, PV = DP + 8;         // LDS row pitches: conflict-free 16-byte rows of K, 4 rows of V half a bank span apart
+    constexpr int NCT = DP / 32, NL = TK * DP / 4 / 256, RSTEP = 1024 / DP;
+    __shared__ __align__(16) float sK[TK * PK];
+    __shared__ __align__(16) float sV[TK * PV];
+    __shared__ int sSpoilt;
+    const int hk = blockIdx.x % a.kv_heads;
+    ServeItem it;
+    if (!serve_item<ROWS_, TK>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
+    const unsigned group = a.heads / a.kv_heads;
+    if (tid == 0) sSpoilt = 0;
+    const auto last_key = [&](int row) { return a.causal ? min(it.p0 + (int)((unsigned)row / group), it.kv - 1) : it.kv - 1; };
+    const int wrow0 = it.row0 + (KS == 1 ? 32 * wave : 0), row = wrow0 + l32;
+    const bool live_row = row < it.rows;
+    const int lim = live_row ? last_key(row) : -1;
+    const int lim_tile0 = last_key(it.row0), lim_tile1 = last_key(min(it.row0 + ROWS_, it.rows) - 1);
+    const int lim_wave1 = wrow0 < it.rows ? last_key(min(wrow0 + 32, it.rows) - 1) : -1;
+    const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
+    const int kt_end = min((int)((int64_t)it.kt * (it.c + 1) / it.nch), (lim_tile1 + TK) / TK);
+
+    const int qrow = min(row, it.rows - 1);   // rows past the end: any row, stored by nobody
+    const int64_t token = it.first + (int)((unsigned)qrow / group), head = hk * (int)group + (int)((unsigned)qrow % group);
+    f32x4 qf[DP / 8];   // features 8s + 4·lh .. +3
+    {
+        const float* Qp = reinterpret_cast<const float*>(a.Q) + token * a.ldq + head * a.dh;
+#pragma unroll
+        for (int s = 0; s < DP / 8; ++s) {
+            const int f = 8 * s + 4 * lh;
+            qf[s] = *reinterpret_cast<const f32x4*>(Qp + (f < a.dh ? f : 0));
+            if (f >= a.dh) qf[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    const int32_t* table = PACKED ? nullptr : a.table + it.seq * a.max_pages;
+    const int page_mask = (1 << a.page_shift) - 1;
+    // page of key kt·TK + half·64 + lane, -1 behind the last key
+    const auto page_of = [&](int kt, int half) {
+        const int key = kt * TK + 64 * half + lane, page = table[min(key, it.kv - 1) >> a.page_shift];
+        return key < it.kv ? page : -1;
+    };
+    const int m_row = tid / (DP / 4), f = 4 * (tid % (DP / 4));   // this thread moves features f .. f+3 of rows i·RSTEP + m_row
+    const int m_f = f < a.dh ? f : 0;
+    typedef typename std::conditional<E4M3, uint32_t, f32x4>::type Piece;
+    Piece kr[NL], vr[NL];
+    int ke[E4M3 ? NL : 1], ve[E4M3 ? NL : 1];
+    const auto load = [&](int kt, int pg0, int pg1) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int r = i * RSTEP + m_row;
+            int64_t kat, vat;
+            if constexpr (PACKED) {
+                const int64_t t = it.first + min(kt * TK + r, it.kv - 1);
+                kat = t * a.ldk + (int64_t)hk * a.dh + m_f;
+                vat = t * a.ldv + (int64_t)hk * a.dh + m_f;
+            } else {
+                const int pg = __shfl(i * RSTEP < 64 ? pg0 : pg1, r & 63), page = (unsigned)pg < (unsigned)a.n_pages ? pg : 0;
+                const int64_t at = (((int64_t)page * a.kv_heads + hk) << a.page_shift) + ((kt * TK + r) & page_mask);
+                if constexpr (E4M3) { ke[i] = a.Ks[at]; ve[i] = a.Vs[at]; }
+                kat = vat = at * a.dh + m_f;
+            }
+            if constexpr (E4M3) {
+                kr[i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(a.K) + kat);
+                vr[i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(a.V) + vat);
+            } else {
+                kr[i] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.K) + kat);
+                vr[i] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.V) + vat);
+            }
+        }
+    };
+    const auto expand = [&](uint32_t c, int byte) {
+        const float s = __uint_as_float(byte ? (uint32_t)byte << 23 : 0x00400000u);
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+        return f32x4{lo[0] * s, lo[1] * s, hi[0] * s, hi[1] * s};
+    };
+    f32x16 o[NCT];
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    // pages of the tile in registers (a, b: its first and second 64 keys) and of the one behind it
+    int pa = 0, pb = 0, na = 0, nb = 0;
+    if (kt_begin < kt_end) {
+        if constexpr (!PACKED) {
+            pa = page_of(kt_begin, 0);
+            na = page_of(kt_begin + 1, 0);
+            if constexpr (KS > 1) { pb = page_of(kt_begin, 1); nb = page_of(kt_begin + 1, 1); }
+        }
+        load(kt_begin, pa, pb);
+    }
+    for (int kt = kt_begin; kt < kt_end; ++kt) {
+        // keys of the stage that are there
+        unsigned long long alive0, alive1 = ~0ull;
+        if constexpr (PACKED) {
+            const int n = it.kv - kt * TK;
+            alive0 = n >= 64 ? ~0ull : (1ull << n) - 1;
+            alive1 = n >= 128 ? ~0ull : n > 64 ? (1ull << (n - 64)) - 1 : 0;
+        } else {
+            alive0 = __builtin_amdgcn_ballot_w64((unsigned)pa < (unsigned)a.n_pages);
+            if constexpr (KS > 1) alive1 = __builtin_amdgcn_ballot_w64((unsigned)pb < (unsigned)a.n_pages);
+        }
+        const bool partial = min(kt * TK + TK, it.kv) - 1 > lim_tile0;   // some row does not see all keys: are their values finite?
+        __syncthreads();
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int r = i * RSTEP + m_row;
+            f32x4 k, v;
+            if constexpr (E4M3) { k = expand(kr[i], ke[i]); v = expand(vr[i], ve[i]); }
+            else { k = kr[i]; v = vr[i]; }
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            if (f >= a.dh) k = v = zero;
+            // a weight of zero does not take NaN away: values of keys that are not there are zeros
+            if (!(((i * RSTEP < 64 ? alive0 : alive1) >> (r & 63)) & 1)) v = zero;
+            *reinterpret_cast<f32x4*>(sK + r * PK + f) = k;
+            *reinterpret_cast<f32x4*>(sV + r * PV + f) = v;
+            if (partial) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top += v[e] * 0.f;   // NaN as soon as one is infinite or NaN
+            }
+        }
+        if (partial && top != 0.f) sSpoilt = 1;
+        __syncthreads();
+        if constexpr (!PACKED) {
+            pa = na; pb = nb;
+            na = page_of(kt + 2, 0);
+            if constexpr (KS > 1) nb = page_of(kt + 2, 1);
+        }
+        if (kt + 1 < kt_end) load(kt + 1, pa, pb);
+        const int kw = KS == 1 ? 0 : wave, key0 = kt * TK + 32 * kw;
+        if (key0 > lim_wave1) continue;
+        f32x16 s;
+        // The matrix instruction adds one product after the other: sums of 16 features, added up, carry less of a rounding error than one chain.
+        constexpr int NU = 2;   // k-groups of 8 in a sum
+#pragma unroll
+        for (int u = 0; u < DP / 8; u += NU) {
+            f32x16 part;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) part[v] = 0.f;
+#pragma unroll
+            for (int w = u; w < u + NU; ++w) {
+                const f32x4 kf = *reinterpret_cast<const f32x4*>(sK + (32 * kw + l32) * PK + 8 * w + 4 * lh);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[w][e], part, 0, 0, 0);
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = u == 0 ? part[v] : s[v] + part[v];
+        }
+        const unsigned alive = (unsigned)((kw < 2 ? alive0 : alive1) >> (32 * (kw & 1)));
+        float mloc = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int key = 8 * (v >> 2) + 4 * lh + (v & 3);
+            s[v] = key0 + key <= lim && ((alive >> key) & 1) ? s[v] : -INFINITY;
+            mloc = fmaxf(mloc, s[v]);
+        }
+        mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
+        const float m_new = fmaxf(m_run, mloc);
+        if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {   // the factor is exactly 1 otherwise
+            const float alpha = m_new > m_run ? expf((m_run - m_new) * a.scale) : 1.f;
+            l_run *= alpha;
+#pragma unroll
+            for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
+            m_run = m_new;
+        }
+        const float m_ref = m_run == -INFINITY ? 0.f : m_run;   // no finite score so far: weights of zero, not -inf - -inf
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            s[v] = expf((s[v] - m_ref) * a.scale);
+            l_run += s[v];
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const float* vrow = sV + (32 * kw + 8 * (v >> 2) + 4 * lh + (v & 3)) * PV + l32;
+#pragma unroll
+            for (int i = 0; i < NCT; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vrow[32 * i], s[v], o[i], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+    if (sSpoilt) {
+        attend_item_by_rows<float, SRC, ROWS_>(a, p, it, hk, kt_begin * TK, kt_end * TK, DP);
+        return;
+    }
+    l_run += __shfl_xor(l_run, 32);
+    if constexpr (KS > 1) {   // waves 2 and 3 hand their sums to waves 0 and 1, wave 1 to wave 0, at the larger maximum
+        constexpr int PER = (NCT * 16 + 2) * 64;
+        static_assert(PER <= TK * PK, "shares fit the stages");
+#pragma unroll
+        for (int half = 2; half >= 1; half >>= 1) {
+            if (wave >= half && wave < 2 * half) {
+                float* share = wave == half ? sK : sV;
+#pragma unroll
+                for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) share[(16 * i + v) * 64 + lane] = o[i][v];
+                share[NCT * 16 * 64 + lane] = m_run;
+                share[(NCT * 16 + 1) * 64 + lane] = l_run;
+            }
+            __syncthreads();
+            if (wave < half) {
+                const float* share = wave == 0 ? sK : sV;
+                const float m_other = share[NCT * 16 * 64 + lane], m_all = fmaxf(m_run, m_other), ref = m_all == -INFINITY ? 0.f : m_all;
+                const float f0 = expf((m_run - ref) * a.scale), f1 = expf((m_other - ref) * a.scale);
+                l_run = l_run * f0 + share[(NCT * 16 + 1) * 64 + lane] * f1;
+                m_run = m_all;
+#pragma unroll
+                for (int i = 0; i < NCT; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[i][v] = fmaf(share[(16 * i + v) * 64 + lane], f1, o[i][v] * f0);
+            }
+            __syncthreads();
+        }
+        if (wave) return;
+    }
+    if (!live_row) return;
+    const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
+    const bool cut = it.nch > 1;   // one of several chunks: sums as they are, with their maximum
+    if (cut && lh == 0) p.part_ml[at] = make_float2(m_run, l_run);
+    const float inv = cut ? 1.f : l_run == 0.f ? 0.f : 1.0f / l_run;
+    float* Op = cut ? p.part_o + at * DP : reinterpret_cast<float*>(a.O) + token * a.ldo + head * a.dh;
+    const int width = cut ? DP : a.dh;
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = 32 * i + 8 * g + 4 * lh;
+            if (c < width) *reinterpret_cast<f32x4*>(Op + c) = f32x4{o[i][4 * g] * inv, o[i][4 * g + 1] * inv, o[i][4 * g + 2] * inv, o[i][4 * g + 3] * inv};
+        }
+}
+
 // Rows whose keys were cut: chunk sums at their common maximum, added in order.  One workgroup per row tile and key head, a thread per row
 // and four features.
 template <typename T, int DP, int ROWS_, int KT_>
@@ -827,6 +1041,11 @@ ServePlan plan_bf16(const ServeArgs& a, bool few) {
     return few ? plan_of(a, ROWS_S, ((int64_t)a.max_kv + KT_S - 1) / KT_S, target, 8) : plan_of(a, ROWS, ((int64_t)a.max_kv + KT - 1) / KT, target, 4);
 }
 
+ServePlan plan_f32(const ServeArgs& a, bool few) {
+    const int target = std::max(1, 512 / a.kv_heads);
+    return few ? plan_of(a, 32, ((int64_t)a.max_kv + 127) / 128, target, 2) : plan_of(a, 128, ((int64_t)a.max_kv + 31) / 32, target, 8);
+}
+
 size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
 
 template <int DP>
@@ -875,18 +1094,40 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool f
     return hipGetLastError();
 }
 
+template <int DP, int KS>
+hipError_t launch_f32(hipStream_t st, const ServeArgs& a, KvSource src, ServePlan p, void* workspace) {
+    p.part_o = reinterpret_cast<float*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.part_rows * a.kv_heads * DP);
+    const int64_t blocks = (int64_t)p.items * a.kv_heads;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks);
+    if (src == KV_PACKED) hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PACKED>), grid, dim3(256), 0, st, a, p);
+    else if (src == KV_PAGED) hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PAGED>), grid, dim3(256), 0, st, a, p);
+    else hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.part_rows) return e;
+    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads));
+    hipLaunchKernelGGL((attn_join_kernel<float, DP, 128 / KS, 32 * KS>), join, dim3(256), 0, st, a, p, a.scale * 1.4426950408889634f);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t serve_attention_workspace(const ServeArgs& a, KvSource, int elem_bytes, int64_t max_new) {
-    if (elem_bytes != 2) return 0;
-    return (part_bytes(a, plan_bf16(a, few_rows(a, max_new))) + 255) & ~(size_t)255;
+    const bool few = few_rows(a, max_new) && (elem_bytes == 2 || a.dh <= 128);
+    return (part_bytes(a, elem_bytes == 2 ? plan_bf16(a, few) : plan_f32(a, few)) + 255) & ~(size_t)255;
 }
 
 hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new, void* workspace) {
-    if (elem_bytes != 2) return launch_rows<float>(st, a, src);
     const int dp = padded_width(a.dh);
-    const bool few = few_rows(a, max_new);
-    return dp == 64 ? launch_tiles<64>(st, a, src, few, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, few, workspace) : launch_tiles<256>(st, a, src, few, workspace);
+    bool few = few_rows(a, max_new);
+    if (elem_bytes == 2)
+        return dp == 64 ? launch_tiles<64>(st, a, src, few, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, few, workspace) : launch_tiles<256>(st, a, src, few, workspace);
+    few = few && dp <= 128;   // (four shares of 256 features do not fit the LDS)
+    const ServePlan p = plan_f32(a, few);
+    if (dp == 64) return few ? launch_f32<64, 4>(st, a, src, p, workspace) : launch_f32<64, 1>(st, a, src, p, workspace);
+    if (dp == 128) return few ? launch_f32<128, 4>(st, a, src, p, workspace) : launch_f32<128, 1>(st, a, src, p, workspace);
+    return launch_f32<256, 1>(st, a, src, p, workspace);
 }
 
 }  // namespace atp
