@@ -469,6 +469,7 @@ class PagedCache:
         self.device = _one_device(K, V, K_scale, V_scale)
         self.K, self.V, self.K_scale, self.V_scale = K, V, K_scale, V_scale
         self.n_pages, self.kv_heads, self.page_size, self.d_h = K.shape
+        self.e4m3 = e4m3
         p = lambda t: None if t is None else t.data_ptr()
         self._c = _Cache(p(K), p(V), p(K_scale), p(V_scale), self.n_pages, self.page_size, self.kv_heads, self.d_h,
                          ATP_CACHE_E4M3 if e4m3 else ATP_CACHE_SAME)
@@ -484,23 +485,27 @@ class PagedCache:
         return cls(codes(), codes(), scale(), scale())
 
 
-def _one_device(*ts) -> torch.device:
-    dev = {t.device for t in ts if t is not None}
-    if len(dev) != 1 or next(iter(dev)).type != "cuda":
+def _one_device(first: torch.Tensor, *ts) -> torch.device:
+    dev = first.device
+    for t in ts:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors must live on one GPU")
+    if dev.type != "cuda":
         raise ValueError("tensors must live on one GPU")
-    return dev.pop()
+    return dev
 
 
 def _rows(t: torch.Tensor, name: str, heads: Optional[int] = None, d_h: Optional[int] = None) -> int:
     """Row stride of a packed [tokens, heads, d_h] tensor, whose rows may be a column block of a wider matrix."""
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (d_h is not None and t.shape[2] != d_h):
+    shape = t.shape
+    if len(shape) != 3 or (heads is not None and shape[1] != heads) or (d_h is not None and shape[2] != d_h):
         raise ValueError(f"{name} must be [tokens, heads, d_h]")
-    row = t.shape[1] * t.shape[2]
-    if t.numel() == 0:
-        return row
-    if (t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError(f"the heads of a row of {name} must lie one behind the other")
-    return t.stride(0) if t.shape[0] > 1 else row
+    n, h, d = shape
+    ld, lh, le = t.stride()
+    if (d > 1 and le != 1) or (h > 1 and lh != d):
+        if n and h and d:
+            raise ValueError(f"the heads of a row of {name} must lie one behind the other")
+    return ld if n > 1 else h * d
 
 
 def _int32(name: str, t: torch.Tensor, dim: int) -> None:
@@ -508,7 +513,7 @@ def _int32(name: str, t: torch.Tensor, dim: int) -> None:
         raise ValueError(f"{name} must be contiguous int32 with {dim} dimension(s)")
 
 
-def _batch(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: int) -> _Batch:
+def _batch(table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: int) -> _Batch:
     _int32("table", table, 2)
     _int32("length", length, 1)
     _int32("offsets", offsets, 1)
@@ -518,21 +523,32 @@ def _batch(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets
     return _Batch(table.data_ptr(), length.data_ptr(), offsets.data_ptr(), n_seq, max_pages, tokens)
 
 
-def _serving(status: int, where: str) -> None:
+def _serve(fn, dev: torch.device, *args) -> None:
+    """One serving call on the current stream of the tensors' device."""
+    if dev.index == torch.cuda.current_device():
+        status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
     if status != 0:
-        raise AtpError(status, where)
+        raise AtpError(status, fn.__name__)
+
+
+def _new_rows(cache: PagedCache, K: torch.Tensor, V: torch.Tensor):
+    """Type and row strides of packed keys and values that go with a cache."""
+    ldk, ldv = _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V", cache.kv_heads, cache.d_h)
+    t = _dt(K)
+    if V.shape[0] != K.shape[0] or V.dtype != K.dtype or (not cache.e4m3 and K.dtype != cache.K.dtype):
+        raise ValueError("K / V shape or dtype mismatch")
+    return t, ldk, ldv
 
 
 def cache_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor) -> None:
     """Rows of the new tokens K, V [tokens, kv_heads, d_h] into their pages: token i of the n new ones of sequence s goes to position
     length[s] - n + i, page table[s, position // page_size].  offsets [n_seq + 1]: where each sequence's tokens start."""
     dev = _one_device(cache.K, K, V, table, length, offsets)
-    ldk, ldv = _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V", cache.kv_heads, cache.d_h)
-    if V.shape != K.shape or V.dtype != K.dtype or cache._c.type == ATP_CACHE_SAME and K.dtype != cache.K.dtype:
-        raise ValueError("K / V shape or dtype mismatch")
-    b = _batch(cache, table, length, offsets, K.shape[0])
-    with torch.cuda.device(dev):
-        _serving(lib.atp_cache_write(cache._c, b, K.data_ptr(), V.data_ptr(), ldk, ldv, _dt(K), _stream()), "atp_cache_write")
+    t, ldk, ldv = _new_rows(cache, K, V)
+    _serve(lib.atp_cache_write, dev, cache._c, _batch(table, length, offsets, K.shape[0]), K.data_ptr(), V.data_ptr(), ldk, ldv, t)
 
 
 def cache_read(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: Optional[int] = None,
@@ -541,19 +557,35 @@ def cache_read(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, off
     outside every sequence stay.  Without it `tokens` (the rows to make, zeros outside every sequence) is wanted, and for an 8-bit cache
     `dtype`."""
     if out is None:
-        if tokens is None or (dtype is None and cache._c.type == ATP_CACHE_E4M3):
+        if tokens is None or (dtype is None and cache.e4m3):
             raise ValueError("without `out`, tokens (and dtype for an 8-bit cache) must be given")
         dt = cache.K.dtype if dtype is None else dtype
         out = tuple(torch.zeros((tokens, cache.kv_heads, cache.d_h), dtype=dt, device=cache.device) for _ in range(2))
     K, V = out
     dev = _one_device(cache.K, K, V, table, length, offsets)
-    ldk, ldv = _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V", cache.kv_heads, cache.d_h)
-    if V.shape != K.shape or V.dtype != K.dtype or cache._c.type == ATP_CACHE_SAME and K.dtype != cache.K.dtype:
-        raise ValueError("K / V shape or dtype mismatch")
-    b = _batch(cache, table, length, offsets, K.shape[0])
-    with torch.cuda.device(dev):
-        _serving(lib.atp_cache_read(cache._c, b, K.data_ptr(), V.data_ptr(), ldk, ldv, _dt(K), _stream()), "atp_cache_read")
+    t, ldk, ldv = _new_rows(cache, K, V)
+    _serve(lib.atp_cache_read, dev, cache._c, _batch(table, length, offsets, K.shape[0]), K.data_ptr(), V.data_ptr(), ldk, ldv, t)
     return K, V
+
+
+def _like_queries(Q: torch.Tensor, out: Optional[torch.Tensor]):
+    """Output rows and their stride."""
+    if out is None:
+        out = torch.zeros(Q.shape, dtype=Q.dtype, device=Q.device)
+    elif out.shape != Q.shape or out.dtype != Q.dtype:
+        raise ValueError("out must have the shape and dtype of Q")
+    return out, _rows(out, "out")
+
+
+def _scratch(need: int, Q: torch.Tensor, workspace: Optional[torch.Tensor]):
+    """(tensor that keeps the workspace alive, its address, its bytes)"""
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=Q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("tensors must be contiguous")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def attention_packed_workspace(n_seq, tokens, heads, kv_heads, d_h, dtype) -> int:
@@ -564,25 +596,18 @@ def attention_packed(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, offsets:
                      workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of packed sequences over their own tokens: Q [tokens, heads, d_h], K, V [tokens, kv_heads, d_h], offsets [n_seq + 1] -> O.
     Rows outside every sequence keep what `out` held (zeros without it)."""
-    dev = _one_device(Q, K, V, offsets, *(t for t in (workspace, out) if t is not None))
+    dev = _one_device(Q, K, V, offsets, workspace, out)
     _int32("offsets", offsets, 1)
-    ldq, ldk = _rows(Q, "Q"), _rows(K, "K", None, Q.shape[2])
-    ldv = _rows(V, "V", K.shape[1], Q.shape[2])
+    ldq, ldk, ldv = _rows(Q, "Q"), _rows(K, "K"), _rows(V, "V")
     tokens, heads, d_h = Q.shape
     kv_heads, n_seq = K.shape[1], offsets.shape[0] - 1
-    if K.shape[0] != tokens or V.shape[0] != tokens or K.dtype != Q.dtype or V.dtype != Q.dtype:
+    if V.shape != K.shape or K.shape[0] != tokens or K.shape[2] != d_h or K.dtype != Q.dtype or V.dtype != Q.dtype:
         raise ValueError("K / V shape or dtype mismatch")
     t = _dt(Q)
-    if out is None:
-        out = torch.zeros((tokens, heads, d_h), dtype=Q.dtype, device=dev)
-    elif out.shape != Q.shape or out.dtype != Q.dtype:
-        raise ValueError("out must have the shape and dtype of Q")
-    ldo = _rows(out, "out")
-    ws = _ws(lib.atp_attention_packed_workspace(n_seq, tokens, heads, kv_heads, d_h, t), Q, workspace)
-    with torch.cuda.device(dev):
-        _serving(lib.atp_attention_packed(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), ldq, ldk, ldv, ldo, offsets.data_ptr(),
-                                          n_seq, tokens, heads, kv_heads, d_h, 1 if causal else 0, float(scale), _ptr(ws),
-                                          0 if ws is None else ws.numel(), t, _stream()), "atp_attention_packed")
+    out, ldo = _like_queries(Q, out)
+    keep, ws, ws_bytes = _scratch(lib.atp_attention_packed_workspace(n_seq, tokens, heads, kv_heads, d_h, t), Q, workspace)
+    _serve(lib.atp_attention_packed, dev, Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), ldq, ldk, ldv, ldo, offsets.data_ptr(),
+           n_seq, tokens, heads, kv_heads, d_h, 1 if causal else 0, scale, ws, ws_bytes, t)
     return out
 
 
@@ -595,22 +620,17 @@ def attention_paged(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the new tokens Q [tokens, heads, d_h] over the pages of their sequence (their own keys are there already).
     max_new: the largest number of new tokens of a sequence, if known (a hint)."""
-    dev = _one_device(cache.K, Q, table, length, offsets, *(t for t in (workspace, out) if t is not None))
+    dev = _one_device(cache.K, Q, table, length, offsets, workspace, out)
     ldq = _rows(Q, "Q", None, cache.d_h)
-    tokens, heads, d_h = Q.shape
     t = _dt(Q)
-    if cache._c.type == ATP_CACHE_SAME and Q.dtype != cache.K.dtype:
+    if not cache.e4m3 and Q.dtype != cache.K.dtype:
         raise ValueError("Q and the cache differ in dtype")
-    if out is None:
-        out = torch.zeros((tokens, heads, d_h), dtype=Q.dtype, device=dev)
-    elif out.shape != Q.shape or out.dtype != Q.dtype:
-        raise ValueError("out must have the shape and dtype of Q")
-    ldo = _rows(out, "out")
-    b = _batch(cache, table, length, offsets, tokens)
-    ws = _ws(lib.atp_attention_paged_workspace(cache._c, b, heads, max_new, t), Q, workspace)
-    with torch.cuda.device(dev):
-        _serving(lib.atp_attention_paged(Q.data_ptr(), cache._c, b, out.data_ptr(), ldq, ldo, heads, 1 if causal else 0, float(scale), max_new,
-                                         _ptr(ws), 0 if ws is None else ws.numel(), t, _stream()), "atp_attention_paged")
+    out, ldo = _like_queries(Q, out)
+    b = _batch(table, length, offsets, Q.shape[0])
+    heads = Q.shape[1]
+    keep, ws, ws_bytes = _scratch(lib.atp_attention_paged_workspace(cache._c, b, heads, max_new, t), Q, workspace)
+    _serve(lib.atp_attention_paged, dev, Q.data_ptr(), cache._c, b, out.data_ptr(), ldq, ldo, heads, 1 if causal else 0, scale, max_new,
+           ws, ws_bytes, t)
     return out
 
 

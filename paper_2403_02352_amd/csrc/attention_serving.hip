@@ -977,53 +977,78 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
         }
 }
 
-// Rows whose keys were cut: chunk sums at their common maximum, added in order.  One workgroup per row tile and key head, a thread per row
-// and four features.
+// Rows whose keys were cut: chunk sums at their common maximum, added in order.  A workgroup takes 8 rows of a row tile of a key head, 32 lanes to
+// a row, which weigh 32 chunks at a time between them and then add up a share of the features each, eight chunks' loads in flight.
+constexpr int JOIN = 8;
+
 template <typename T, int DP, int ROWS_, int KT_>
 __global__ void __launch_bounds__(256) attn_join_kernel(ServeArgs a, ServePlan p, float c_log2e) {
+    constexpr int NF = DP / 32;   // features of a lane
+    typedef float Share __attribute__((ext_vector_type(NF)));
     const int hk = blockIdx.x % a.kv_heads;
     ServeItem it;
     if (!serve_item<ROWS_, KT_>(a, p, blockIdx.x / a.kv_heads, false, it) || it.nch < 2) return;
     const unsigned group = a.heads / a.kv_heads;
-    const int end = min(ROWS_, it.rows - it.row0) * (DP / 4);
-    for (int x = threadIdx.x; x < end; x += 256) {
-        const int row = it.row0 + x / (DP / 4), f = 4 * (x % (DP / 4));
-        const int64_t at = (int64_t)hk * p.part_rows + it.part + row;
-        float m = -INFINITY;
-        for (int c = 0; c < it.nch; ++c) m = fmaxf(m, p.part_ml[at + (int64_t)c * it.rows].x);
-        const float ref = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < it.nch; ++c) {
-            const float2 ml = p.part_ml[at + (int64_t)c * it.rows];
-            const float w = __builtin_amdgcn_exp2f((ml.x - ref) * c_log2e);
-            if (w == 0.f) continue;
-            l = fmaf(ml.y, w, l);
-            const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (at + (int64_t)c * it.rows) * DP + f);
+    const int l32 = threadIdx.x & 31, row = it.row0 + JOIN * (int)blockIdx.y + (int)(threadIdx.x >> 5);
+    if (row >= it.rows) return;   // (whole halves of a wave: the exchanges below stay within one)
+    const int64_t at = (int64_t)hk * p.part_rows + it.part + row;
+    float m = -INFINITY;
+    for (int c = l32; c < it.nch; c += 32) m = fmaxf(m, p.part_ml[at + (int64_t)c * it.rows].x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], w, o[e]);
+    for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 32));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    Share o;
+#pragma unroll
+    for (int e = 0; e < NF; ++e) o[e] = 0.f;
+    for (int c0 = 0; c0 < it.nch; c0 += 32) {
+        float w = 0.f, lw = 0.f;
+        if (c0 + l32 < it.nch) {
+            const float2 ml = p.part_ml[at + (int64_t)(c0 + l32) * it.rows];
+            w = __builtin_amdgcn_exp2f((ml.x - ref) * c_log2e);
+            lw = w == 0.f ? 0.f : ml.y * w;
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        if (f >= a.dh) continue;
-        const int64_t t = it.first + (int)((unsigned)row / group), h = hk * (int)group + (int)((unsigned)row % group);
-        T* Op = reinterpret_cast<T*>(a.O) + t * a.ldo + h * a.dh + f;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(Op) = make_uint2(pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv));
-        else *reinterpret_cast<f32x4*>(Op) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        const int n = min(32, it.nch - c0);
+        for (int c = 0; c < n; c += 8) {
+            Share v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const Share*>(p.part_o + (at + (int64_t)(c0 + min(c + k, n - 1)) * it.rows) * DP + NF * l32);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float wk = __shfl(w, c + k, 32);   // (zero behind the last chunk)
+                l += __shfl(lw, c + k, 32);
+#pragma unroll
+                for (int e = 0; e < NF; ++e) o[e] = wk == 0.f ? o[e] : fmaf(v[k][e], wk, o[e]);
+            }
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t t = it.first + (int)((unsigned)row / group), h = hk * (int)group + (int)((unsigned)row % group);
+    T* Op = reinterpret_cast<T*>(a.O) + t * a.ldo + h * a.dh;
+#pragma unroll
+    for (int e = 0; e < NF; e += 2) {
+        const int f = NF * l32 + e;   // (d_h is even)
+        if (f >= a.dh) break;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(Op + f) = pack_bf2(o[e] * inv, o[e + 1] * inv);
+        else *reinterpret_cast<f32x2*>(Op + f) = f32x2{o[e] * inv, o[e + 1] * inv};
     }
 }
 
 // Items and partial rows that the lengths on the device can lead to, from the sizes that the host knows.  With chunks of at least
-// total / target tiles a cut sequence has fewer than 2·tiles/chunk chunks, so all cut row tiles together have fewer than 2·target.
-ServePlan plan_of(const ServeArgs& a, int64_t rows, int64_t kt, int target, int min_chunk) {
+// total / target tiles a cut sequence has fewer than 2·tiles/chunk chunks, so all cut row tiles together have fewer than 2·target.  Keys are not
+// cut where the row tiles of the tokens fill the chip by themselves: no partial rows, no second launch.
+ServePlan plan_of(const ServeArgs& a, int rows, int kt, int wanted, int min_chunk) {
     ServePlan p;
-    p.target = target;
-    p.min_chunk = min_chunk;
-    const int64_t all_rows = (int64_t)a.tokens * (a.heads / a.kv_heads);
+    const int64_t all_rows = (int64_t)a.tokens * (a.heads / a.kv_heads), key_tiles = ((int64_t)a.max_kv + kt - 1) / kt;
     const int64_t tiles = all_rows / rows + std::min<int64_t>(a.n_seq, a.tokens);
-    const int64_t cuts = std::min<int64_t>((kt + min_chunk - 1) / min_chunk, 2 * target);
+    const int64_t target = std::max(1, wanted / a.kv_heads);
+    const bool cut = all_rows / rows < target && key_tiles > min_chunk;
+    const int64_t cuts = cut ? std::min<int64_t>((key_tiles + min_chunk - 1) / min_chunk, 2 * target) : 1;
+    p.target = cut ? (int)target : 1;
+    p.min_chunk = cut ? min_chunk : 1 << 30;
     p.tiles = (int)tiles;
-    p.items = (int)std::min(tiles + target, tiles * cuts);
-    p.part_rows = cuts < 2 ? 0 : std::min<int64_t>(2 * target * rows, cuts * all_rows);
+    p.items = (int)(cut ? std::min(tiles + target, tiles * cuts) : tiles);
+    p.part_rows = cut ? std::min<int64_t>(2 * target * rows, cuts * all_rows) : 0;
     return p;
 }
 
@@ -1037,14 +1062,10 @@ bool few_rows(const ServeArgs& a, int64_t max_new) {
 }
 
 ServePlan plan_bf16(const ServeArgs& a, bool few) {
-    const int target = std::max(1, 1024 / a.kv_heads);
-    return few ? plan_of(a, ROWS_S, ((int64_t)a.max_kv + KT_S - 1) / KT_S, target, 8) : plan_of(a, ROWS, ((int64_t)a.max_kv + KT - 1) / KT, target, 4);
+    return few ? plan_of(a, ROWS_S, KT_S, 1024, 16) : plan_of(a, ROWS, KT, 1024, 4);
 }
 
-ServePlan plan_f32(const ServeArgs& a, bool few) {
-    const int target = std::max(1, 512 / a.kv_heads);
-    return few ? plan_of(a, 32, ((int64_t)a.max_kv + 127) / 128, target, 2) : plan_of(a, 128, ((int64_t)a.max_kv + 31) / 32, target, 8);
-}
+ServePlan plan_f32(const ServeArgs& a, bool few) { return few ? plan_of(a, 32, 128, 512, 2) : plan_of(a, 128, 32, 512, 8); }
 
 size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
 
@@ -1088,7 +1109,7 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool f
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part_rows) return e;
-    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads));
+    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads), (few ? ROWS_S : ROWS) / JOIN);
     if (few) hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS_S, KT_S>), join, dim3(256), 0, st, a, p, c);
     else hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS, KT>), join, dim3(256), 0, st, a, p, c);
     return hipGetLastError();
@@ -1106,7 +1127,7 @@ hipError_t launch_f32(hipStream_t st, const ServeArgs& a, KvSource src, ServePla
     else hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part_rows) return e;
-    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads));
+    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads), 128 / KS / JOIN);
     hipLaunchKernelGGL((attn_join_kernel<float, DP, 128 / KS, 32 * KS>), join, dim3(256), 0, st, a, p, a.scale * 1.4426950408889634f);
     return hipGetLastError();
 }
