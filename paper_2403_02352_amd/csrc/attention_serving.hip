@@ -295,15 +295,16 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     const auto compute = [&](int kt, const uint4* K, const uint4* V, unsigned long long alive) {
         f32x16 s[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int v = 0; v < 16; ++v) s[t][v] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) {
+        for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {   // (two chains of sums side by side)
                 const bf16x8 kf = u4_as_bf16x8(K[(32 * t + prow) * CK + ((2 * ks + lh) ^ pswz)]);
                 s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[t], 0, 0, 0);
             }
-        }
         if (kt * KT + KT - 1 > lim_wave0 || alive != ~0ull) {   // some row of this wave does not see all keys
 #pragma unroll
             for (int t = 0; t < NT; ++t) {

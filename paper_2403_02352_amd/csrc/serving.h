@@ -74,31 +74,38 @@ __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& 
     };
     const auto row_tiles = [&] { return (int)(((unsigned)n * group + ROWS - 1) / ROWS); };
     const auto key_tiles = [&] { return max((kv + KT - 1) / KT, 1); };
-    long long total = 0;
-    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        look(s0 + lane);
-        total += (long long)row_tiles() * key_tiles();
+    const int steps = min(a.n_seq, 64);   // (lanes from n_seq on hold nothing: the exchanges stop there)
+    const bool cut = p.part_rows > 0;
+    int chunk = 1 << 30;
+    if (cut) {
+        // (in floats, a little more than the share: the bound on the cuts holds whatever the sum's rounding)
+        float total = 0.f;
+        for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+            look(s0 + lane);
+            total += (float)row_tiles() * (float)key_tiles();
+        }
+        for (int off = 1; off < steps; off <<= 1) total += __shfl_xor(total, off);
+        const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(total)));
+        chunk = max((int)fminf(all * 1.00001f / (float)p.target + 1.f, 1e9f), p.min_chunk);
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
-    const long long even = (total + p.target - 1) / p.target;
-    const int chunk = (int)min(max(even, (long long)p.min_chunk), (long long)(1 << 30));
     int before = 0;
-    long long part = 0;
+    int64_t part = 0;
     for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        if (a.n_seq > 64) look(s0 + lane);
+        if (!cut || a.n_seq > 64) look(s0 + lane);
         const int kt = key_tiles(), nch = (kt + chunk - 1) / chunk, rt = row_tiles();
         const int mine = chunks ? rt * nch : rt;
-        const long long mine_part = nch > 1 ? (long long)((unsigned)n * group) * nch : 0;
-        int upto = mine;
-        long long upto_part = mine_part;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
+        const int mine_part = nch > 1 ? (int)min((int64_t)((unsigned)n * group) * nch, (int64_t)1 << 24) : 0;
+        int upto = mine, upto_part = mine_part;
+        for (int off = 1; off < steps; off <<= 1) {
             const int x = __shfl_up(upto, off);
-            const long long y = __shfl_up(upto_part, off);
-            if (lane >= off) { upto += x; upto_part += y; }
+            if (lane >= off) upto += x;
         }
-        const unsigned long long behind = __builtin_amdgcn_ballot_w64(before + upto > w);
+        if (cut)
+            for (int off = 1; off < steps; off <<= 1) {
+                const int y = __shfl_up(upto_part, off);
+                if (lane >= off) upto_part += y;
+            }
+        const unsigned long long behind = __builtin_amdgcn_ballot_w64(lane < steps && before + upto > w);
         if (behind) {
             const int at = __builtin_ctzll(behind);
             const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
@@ -110,14 +117,12 @@ __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& 
             const int local = w - before - of(upto - mine), per = chunks ? it.nch : 1;
             it.row0 = (of(rt) - 1 - local / per) * ROWS;
             it.c = local % per;
-            const long long pb = part + upto_part - mine_part;
-            it.part = (long long)(((unsigned long long)(unsigned)of((int)(pb >> 32)) << 32) | (unsigned)of((int)pb));
+            it.part = part + of(upto_part - mine_part);
             // (offsets that decrease can count more rows than there are: no item for what the grid and the workspace do not hold)
             return local >= 0 && local < of(mine) && (it.nch == 1 || it.part + (int64_t)it.rows * it.nch <= p.part_rows);
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
-        const long long last = __shfl(upto_part, 63);
-        part += last;
+        before += __builtin_amdgcn_readlane(upto, steps - 1);
+        part += __builtin_amdgcn_readlane(upto_part, steps - 1);
     }
     return false;
 }
