@@ -1043,7 +1043,7 @@ ServePlan plan_of(const ServeArgs& a, int rows, int kt, int wanted, int min_chun
     const int64_t all_rows = (int64_t)a.tokens * (a.heads / a.kv_heads), key_tiles = ((int64_t)a.max_kv + kt - 1) / kt;
     const int64_t tiles = all_rows / rows + std::min<int64_t>(a.n_seq, a.tokens);
     const int64_t target = std::max(1, wanted / a.kv_heads);
-    const bool cut = all_rows / rows < target && key_tiles > min_chunk;
+    const bool cut = all_rows / rows < target && a.max_kv > 512;   // (up to 512 keys the second launch costs more than it saves)
     const int64_t cuts = cut ? std::min<int64_t>((key_tiles + min_chunk - 1) / min_chunk, 2 * target) : 1;
     p.target = cut ? (int)target : 1;
     p.min_chunk = cut ? min_chunk : 1 << 30;
@@ -1062,11 +1062,11 @@ bool few_rows(const ServeArgs& a, int64_t max_new) {
     return rows <= ROWS_S;
 }
 
-ServePlan plan_bf16(const ServeArgs& a, bool few) {
-    return few ? plan_of(a, ROWS_S, KT_S, 1024, 16) : plan_of(a, ROWS, KT, 1024, 4);
-}
-
-ServePlan plan_f32(const ServeArgs& a, bool few) { return few ? plan_of(a, 32, 128, 512, 2) : plan_of(a, 128, 32, 512, 8); }
+// (wanted items and smallest chunk by measurement, us: 64 sequences of 256 to 8192 keys, e4m3, 512 / 768 / 1024 / 1536 / 2048 items 81 / 80 / 83 / 89 / 90,
+// 6 of 16384 to 65536 keys 199 / 190 / 190 / 179 / 185, 32 of 100 to 20000 82 / 75 / 82 / 84 / 91; one of 32768 keys in chunks of at least 256 / 512 keys
+// 40 / 29; 1238 new tokens over 3000 to 16384 keys, 1024 items of at least 256 / 512 keys 287 / 279; fp32, 150 over 100 to 2000, at least 128 / 256 keys 28 / 43)
+ServePlan plan_bf16(const ServeArgs& a, bool few) { return few ? plan_of(a, ROWS_S, KT_S, 768, 16) : plan_of(a, ROWS, KT, 1024, 8); }
+ServePlan plan_f32(const ServeArgs& a, bool few) { return few ? plan_of(a, 32, 128, 512, 2) : plan_of(a, 128, 32, 512, 4); }
 
 size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
 
