@@ -1055,11 +1055,12 @@ ServePlan plan_of(const ServeArgs& a, int rows, int kt, int wanted, int min_chun
 
 int padded_width(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 
-// Few rows a sequence (by what the caller says, else on average): the kernel of 32 rows.
-bool few_rows(const ServeArgs& a, int64_t max_new) {
-    const int64_t group = a.heads / a.kv_heads;
-    const int64_t rows = max_new > 0 ? std::min<int64_t>(max_new, a.tokens) * group : ((int64_t)a.tokens + a.n_seq - 1) / a.n_seq * group;
-    return rows <= ROWS_S;
+// Few rows a sequence, on average or at most by what the caller says: the kernel of 32 rows.  bf16, us, tiles of 128 / of 32, 16 sequences of 4096
+// keys and 64 of 1024: 36 rows 63 / 70 and 81 / 70, 64 rows 73 / 72 and 93 / 65, 96 rows 81 / 92 and 105 / 89, 128 rows 97 / 121 and 126 / 120; e4m3,
+// 64 rows 59 / 53 and 79 / 45, 128 rows 73 / 83 and 102 / 82; 63 single tokens and a chunk of 512, 36 rows on average, 280 / 263 and 222 / 173.
+bool few_rows(const ServeArgs& a, int elem_bytes, int64_t max_new) {
+    const int64_t group = a.heads / a.kv_heads, most = elem_bytes == 2 ? 64 : 32;
+    return (max_new > 0 && max_new <= most / group) || a.tokens * group <= most * a.n_seq;
 }
 
 // (wanted items and smallest chunk by measurement, us: 64 sequences of 256 to 8192 keys, e4m3, 512 / 768 / 1024 / 1536 / 2048 items 81 / 80 / 83 / 89 / 90,
@@ -1136,13 +1137,13 @@ hipError_t launch_f32(hipStream_t st, const ServeArgs& a, KvSource src, ServePla
 }  // namespace
 
 size_t serve_attention_workspace(const ServeArgs& a, KvSource, int elem_bytes, int64_t max_new) {
-    const bool few = few_rows(a, max_new) && (elem_bytes == 2 || a.dh <= 128);
+    const bool few = few_rows(a, elem_bytes, max_new) && (elem_bytes == 2 || a.dh <= 128);
     return (part_bytes(a, elem_bytes == 2 ? plan_bf16(a, few) : plan_f32(a, few)) + 255) & ~(size_t)255;
 }
 
 hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new, void* workspace) {
     const int dp = padded_width(a.dh);
-    bool few = few_rows(a, max_new);
+    bool few = few_rows(a, elem_bytes, max_new);
     if (elem_bytes == 2)
         return dp == 64 ? launch_tiles<64>(st, a, src, few, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, few, workspace) : launch_tiles<256>(st, a, src, few, workspace);
     few = few && dp <= 128;   // (four shares of 256 features do not fit the LDS)
