@@ -455,23 +455,24 @@ class PagedCache:
     codes with a biased exponent (uint8 [n_pages, kv_heads, page_size]) for every row.  The tensors stay the caller's."""
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: Optional[torch.Tensor] = None, V_scale: Optional[torch.Tensor] = None):
-        _check(K, V, K_scale, V_scale)
-        e4m3 = K.dtype == torch.float8_e4m3fn
-        if K.dim() != 4 or V.shape != K.shape or V.dtype != K.dtype:
+        e4m3, shape = K.dtype == torch.float8_e4m3fn, K.shape
+        if len(shape) != 4 or V.shape != shape or V.dtype != K.dtype:
             raise ValueError("K and V must be [n_pages, kv_heads, page_size, d_h] of one type")
         if not e4m3:
             _dt(K)
-        for s in (K_scale, V_scale):
-            if (s is not None) != e4m3:
-                raise ValueError("float8_e4m3fn pages have scales, others none")
-            if s is not None and (s.dtype != torch.uint8 or s.shape != K.shape[:3]):
-                raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
+        if (K_scale is not None) != e4m3 or (V_scale is not None) != e4m3:
+            raise ValueError("float8_e4m3fn pages have scales, others none")
         self.device = _one_device(K, V, K_scale, V_scale)
-        self.K, self.V, self.K_scale, self.V_scale = K, V, K_scale, V_scale
-        self.n_pages, self.kv_heads, self.page_size, self.d_h = K.shape
-        self.e4m3 = e4m3
-        p = lambda t: None if t is None else t.data_ptr()
-        self._c = _Cache(p(K), p(V), p(K_scale), p(V_scale), self.n_pages, self.page_size, self.kv_heads, self.d_h,
+        _check(K, V, K_scale, V_scale)
+        self.K, self.V, self.K_scale, self.V_scale, self.e4m3 = K, V, K_scale, V_scale, e4m3
+        self.n_pages, self.kv_heads, self.page_size, self.d_h = shape
+        ks = vs = None
+        if e4m3:
+            for s in (K_scale, V_scale):
+                if s.dtype != torch.uint8 or s.shape != shape[:3]:
+                    raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
+            ks, vs = K_scale.data_ptr(), V_scale.data_ptr()
+        self._c = _Cache(K.data_ptr(), V.data_ptr(), ks, vs, self.n_pages, self.page_size, self.kv_heads, self.d_h,
                          ATP_CACHE_E4M3 if e4m3 else ATP_CACHE_SAME)
 
     @classmethod
@@ -525,11 +526,12 @@ def _batch(table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tok
 
 def _serve(fn, dev: torch.device, *args) -> None:
     """One serving call on the current stream of the tensors' device."""
+    stream = torch._C._cuda_getCurrentRawStream(dev.index)   # (the handle alone: the stream object costs a microsecond of a step's dozen)
     if dev.index == torch.cuda.current_device():
-        status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+        status = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            status = fn(*args, stream)
     if status != 0:
         raise AtpError(status, fn.__name__)
 
