@@ -1059,8 +1059,11 @@ int padded_width(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 // keys and 64 of 1024: 36 rows 63 / 70 and 81 / 70, 64 rows 73 / 72 and 93 / 65, 96 rows 81 / 92 and 105 / 89, 128 rows 97 / 121 and 126 / 120; e4m3,
 // 64 rows 59 / 53 and 79 / 45, 128 rows 73 / 83 and 102 / 82; 63 single tokens and a chunk of 512, 36 rows on average, 280 / 263 and 222 / 173.
 bool few_rows(const ServeArgs& a, int elem_bytes, int64_t max_new) {
-    const int64_t group = a.heads / a.kv_heads, most = elem_bytes == 2 ? 64 : 32;
-    return (max_new > 0 && max_new <= most / group) || a.tokens * group <= most * a.n_seq;
+    const int64_t group = a.heads / a.kv_heads, most = elem_bytes == 2 ? 64 : 32, rows = a.tokens * group;
+    if ((max_new > 0 && max_new <= most / group) || rows <= most * a.n_seq) return true;
+    // fp32 over a few keys, as long as tiles of 32 rows are one round of workgroups: their four waves go through the keys at once instead of one after
+    // the other (12 heads of 64, us, tiles of 128 / of 32: 5 prompts of 96 tokens 18.3 / 11.5, of 48 14.0 / 11.4; 16 of 128, two rounds, 22.8 / 31.7)
+    return elem_bytes == 4 && a.max_kv <= 512 && (rows / 32 + a.n_seq) * a.kv_heads <= 256;
 }
 
 // (wanted items and smallest chunk by measurement, us: 64 sequences of 256 to 8192 keys, e4m3, 512 / 768 / 1024 / 1536 / 2048 items 81 / 80 / 83 / 89 / 90,
