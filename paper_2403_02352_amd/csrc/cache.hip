@@ -48,19 +48,37 @@ __device__ __forceinline__ void store8(T* p, const Octet& o) {
     }
 }
 
-// One wave per token and slice of its rows: the 2·kv_heads rows of a token (keys, then values) are cut into pieces of 8 elements, 1 << gs lanes
-// to a row (the power of two that holds d_h / 8), PER wave-fuls of pieces to a wave.  The token's place is found once per wave.
-// Bound by memory for prompts (each element read once and written once), by the chain search - table - row for the tokens of a step.
+// One wave per token and slice of its rows: the 2·kv_heads rows of a token (keys, then values) are cut into pieces of 8 elements, 1 << GS lanes
+// to a row (the power of two that holds d_h / 8), PER wave-fuls of pieces to a wave.  The token's place is found once per wave, while its new rows are
+// on their way: where they come from depends on nothing else.
+// Bound by memory for prompts (each element read once and written once), by the chain offsets - table - row for the tokens of a step.
 constexpr int PER = 4;
 
-template <typename T, bool E4M3, bool WRITE>
-__global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a, int gs) {
+template <typename T, bool E4M3, bool WRITE, int GS>
+__global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a) {
+    constexpr int RPW = 64 >> GS;                                    // rows of a wave-ful
     const int lane = threadIdx.x & 63;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int rows_per = 64 >> gs;                                   // rows of a wave-ful
-    const int slices = (2 * a.kv_heads + PER * rows_per - 1) / (PER * rows_per);
+    const int slices = (2 * a.kv_heads + PER * RPW - 1) / (PER * RPW);
     const int token = __builtin_amdgcn_readfirstlane((int)(w / slices)), slice = __builtin_amdgcn_readfirstlane((int)(w % slices));
     if (token >= a.tokens) return;
+    const int piece = lane & ((1 << GS) - 1);
+    bool live[PER], key[PER];
+    int h[PER];
+    int64_t packed[PER];   // where the piece lies in the packed rows (of some other where there is none: loads are unconditional)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int row = (slice * PER + i) * RPW + (lane >> GS);
+        live[i] = row < 2 * a.kv_heads && piece * 8 < a.dh;
+        key[i] = row < a.kv_heads || !live[i];
+        h[i] = !live[i] ? 0 : key[i] ? row : row - a.kv_heads;
+        packed[i] = (int64_t)token * (key[i] ? a.ldk : a.ldv) + (int64_t)h[i] * a.dh + (live[i] ? piece * 8 : 0);
+    }
+    Octet o[PER];
+    if constexpr (WRITE) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) o[i] = load8(reinterpret_cast<const T*>(key[i] ? a.Kn : a.Vn) + packed[i]);
+    }
     const int s = sequence_of(a, token);
     if (s < 0) return;
     int first, n;
@@ -69,77 +87,91 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a, int gs) {
     int page = -1;
     if (pos >= 0 && pos < a.max_kv) page = a.table[s * a.max_pages + (pos >> a.page_shift)];
     const bool placed = page >= 0 && page < a.n_pages;
-    if (WRITE && !placed) return;
     const int slot = pos & ((1 << a.page_shift) - 1);
-    const int piece = lane & ((1 << gs) - 1);
-    const bool inside = piece * 8 < a.dh;
+    int64_t at[PER];   // row of the cache
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int row = (slice * PER + i) * rows_per + (lane >> gs);
-        const bool live = row < 2 * a.kv_heads && inside;
-        const bool key = row < a.kv_heads;
-        const int h = key ? row : row - a.kv_heads;
-        const int64_t at = (((int64_t)page * a.kv_heads + h) << a.page_shift) + slot;
-        const int64_t packed = (int64_t)token * (key ? a.ldk : a.ldv) + (int64_t)h * a.dh + piece * 8;
-        Octet o = {};
-        if constexpr (WRITE) {
-            if (live) o = load8(reinterpret_cast<const T*>(key ? a.Kn : a.Vn) + packed);
+    for (int i = 0; i < PER; ++i) at[i] = (((int64_t)(placed ? page : 0) * a.kv_heads + h[i]) << a.page_shift) + (placed ? slot : 0);
+    if constexpr (WRITE) {
+        if (!placed) return;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
             if constexpr (E4M3) {
                 float top = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float m = fabsf(o.v[e]);
-                    top = fmaxf(top, m < INFINITY ? m : 0.f);
+                    const float m = fabsf(o[i].v[e]);
+                    top = fmaxf(top, m < INFINITY && live[i] ? m : 0.f);
                 }
-                for (int off = 1; off < (1 << gs); off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+#pragma unroll
+                for (int off = 1; off < (1 << GS); off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
                 const int byte = row_exponent(top);
                 const float f = byte ? inverse_scale_of(byte) : 0x1p127f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o.v[e] = fabsf(o.v[e]) < INFINITY ? o.v[e] * f : NAN;
-                if (live) {
-                    *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(key ? a.K : a.V) + at * a.dh + piece * 8) =
-                        make_uint2(pack_e4m3(o.v[0], o.v[1], o.v[2], o.v[3]), pack_e4m3(o.v[4], o.v[5], o.v[6], o.v[7]));
-                    if (piece == 0) (key ? a.Ks : a.Vs)[at] = (uint8_t)byte;
+                for (int e = 0; e < 8; ++e) o[i].v[e] = fabsf(o[i].v[e]) < INFINITY ? o[i].v[e] * f : NAN;
+                if (live[i]) {
+                    *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(key[i] ? a.K : a.V) + at[i] * a.dh + piece * 8) =
+                        make_uint2(pack_e4m3(o[i].v[0], o[i].v[1], o[i].v[2], o[i].v[3]), pack_e4m3(o[i].v[4], o[i].v[5], o[i].v[6], o[i].v[7]));
+                    if (piece == 0) (key[i] ? a.Ks : a.Vs)[at[i]] = (uint8_t)byte;
                 }
-            } else {
-                if (live) store8(reinterpret_cast<T*>(key ? a.K : a.V) + at * a.dh + piece * 8, o);
+            } else if (live[i]) {
+                store8(reinterpret_cast<T*>(key[i] ? a.K : a.V) + at[i] * a.dh + piece * 8, o[i]);
+            }
+        }
+    } else {
+        const int f8 = piece * 8 < a.dh ? piece * 8 : 0;
+        if constexpr (E4M3) {
+            uint2 c[PER];
+            int byte[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                c[i] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(key[i] ? a.K : a.V) + at[i] * a.dh + f8);
+                byte[i] = (key[i] ? a.Ks : a.Vs)[at[i]];
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const float f = scale_of(byte[i]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)(e ? c[i].y : c[i].x), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)(e ? c[i].y : c[i].x), true);
+                    o[i].v[4 * e] = lo[0] * f; o[i].v[4 * e + 1] = lo[1] * f; o[i].v[4 * e + 2] = hi[0] * f; o[i].v[4 * e + 3] = hi[1] * f;
+                }
             }
         } else {
-            if (live && placed) {
-                if constexpr (E4M3) {
-                    const uint2 c = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(key ? a.K : a.V) + at * a.dh + piece * 8);
-                    const float f = scale_of((key ? a.Ks : a.Vs)[at]);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)(e ? c.y : c.x), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)(e ? c.y : c.x), true);
-                        o.v[4 * e] = lo[0] * f; o.v[4 * e + 1] = lo[1] * f; o.v[4 * e + 2] = hi[0] * f; o.v[4 * e + 3] = hi[1] * f;
-                    }
-                } else {
-                    o = load8(reinterpret_cast<const T*>(key ? a.K : a.V) + at * a.dh + piece * 8);
-                }
-            }
-            if (live) store8(reinterpret_cast<T*>(key ? a.Ko : a.Vo) + packed, o);
+            for (int i = 0; i < PER; ++i) o[i] = load8(reinterpret_cast<const T*>(key[i] ? a.K : a.V) + at[i] * a.dh + f8);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[i].v[e] = placed ? o[i].v[e] : 0.f;
+            if (live[i]) store8(reinterpret_cast<T*>(key[i] ? a.Ko : a.Vo) + packed[i], o[i]);
         }
     }
 }
 
-template <bool WRITE>
-hipError_t launch_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3) {
-    int gs = 0;
-    while ((8 << gs) < a.dh) ++gs;
-    const int rows_per = 64 >> gs;
-    const int64_t slices = (2 * a.kv_heads + PER * rows_per - 1) / (PER * rows_per);
+template <bool WRITE, int GS>
+hipError_t launch_group(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3) {
+    constexpr int RPW = 64 >> GS;
+    const int64_t slices = (2 * (int64_t)a.kv_heads + PER * RPW - 1) / (PER * RPW);
     const int64_t blocks = ((int64_t)a.tokens * slices + 3) / 4;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
     if (elem_bytes == 2) {
-        if (e4m3) hipLaunchKernelGGL((cache_rows_kernel<bf16_t, true, WRITE>), grid, dim3(256), 0, st, a, gs);
-        else hipLaunchKernelGGL((cache_rows_kernel<bf16_t, false, WRITE>), grid, dim3(256), 0, st, a, gs);
+        if (e4m3) hipLaunchKernelGGL((cache_rows_kernel<bf16_t, true, WRITE, GS>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((cache_rows_kernel<bf16_t, false, WRITE, GS>), grid, dim3(256), 0, st, a);
     } else {
-        if (e4m3) hipLaunchKernelGGL((cache_rows_kernel<float, true, WRITE>), grid, dim3(256), 0, st, a, gs);
-        else hipLaunchKernelGGL((cache_rows_kernel<float, false, WRITE>), grid, dim3(256), 0, st, a, gs);
+        if (e4m3) hipLaunchKernelGGL((cache_rows_kernel<float, true, WRITE, GS>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((cache_rows_kernel<float, false, WRITE, GS>), grid, dim3(256), 0, st, a);
     }
     return hipGetLastError();
+}
+
+template <bool WRITE>
+hipError_t launch_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3) {
+    // (rows of 8 to 64 elements share 8 lanes: narrower heads than that are rare)
+    if (a.dh <= 64) return launch_group<WRITE, 3>(st, a, elem_bytes, e4m3);
+    if (a.dh <= 128) return launch_group<WRITE, 4>(st, a, elem_bytes, e4m3);
+    return launch_group<WRITE, 5>(st, a, elem_bytes, e4m3);
 }
 
 }  // namespace
