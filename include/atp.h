@@ -390,7 +390,7 @@ atp_status atp_norm_factored(const void* P, const void* C, const float* gain, fl
  * each sequence starts: tokens offsets[s] … offsets[s+1] − 1 belong to sequence s (none when both are equal).  Rows outside every sequence
  * are not written, and what they hold reaches nobody.  A token's row of heads·d_h elements is contiguous, rows are a stride (ldq, ldk, ldv, ldo, in elements)
  * apart, so Q, K and V may be column blocks of one packed projection.  Every stride is a multiple of 16 bytes and at least the row.
- * `heads` is a multiple of `kv_heads`: query head h reads key head h / (heads / kv_heads).  d_h is a multiple of 8 up to 256.
+ * At most 65536 sequences a call.  `heads` is a multiple of `kv_heads`: query head h reads key head h / (heads / kv_heads).  d_h is a multiple of 8 up to 256.
  * Offsets are read on the device only: they may change between replays of a captured graph, as long as `tokens` and `n_seq` stay.
  * Values outside 0 … tokens are taken to the nearest bound, a sequence that ends before it starts is empty, and the sequences of offsets
  * that decrease are computed in an undefined way, within the tensors.

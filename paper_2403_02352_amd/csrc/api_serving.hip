@@ -6,6 +6,8 @@ using namespace atp;
 
 namespace {
 
+constexpr int64_t MAX_SEQ = 65536;   // (every workgroup counts the sequences up)
+
 // what the checks of a cache and a batch leave in the arguments of a kernel
 atp_status take_cache(const atp_cache* c, const atp_batch* b, const atp_dtype& t, ServeArgs& a, bool pointers) {
     if (!c || !b || bad_dtype(t)) return ATP_ERR_INVALID_ARG;
@@ -13,7 +15,7 @@ atp_status take_cache(const atp_cache* c, const atp_batch* b, const atp_dtype& t
     if (type != ATP_CACHE_SAME && type != ATP_CACHE_E4M3) return ATP_ERR_INVALID_ARG;
     if (c->n_pages < 1 || c->n_pages > 0x7fffffff || c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) || c->kv_heads < 1 || c->d_h < 1)
         return ATP_ERR_INVALID_ARG;
-    if (b->n_seq < 1 || b->n_seq > (1 << 24) || b->max_pages < 1 || b->tokens < 0 || b->tokens > 0x7fffffff) return ATP_ERR_INVALID_ARG;
+    if (b->n_seq < 1 || b->n_seq > MAX_SEQ || b->max_pages < 1 || b->tokens < 0 || b->tokens > 0x7fffffff) return ATP_ERR_INVALID_ARG;
     if (c->d_h % 8 || c->d_h > 256 || c->kv_heads > 65535) return ATP_ERR_UNSUPPORTED;
     if (b->max_pages > (1 << 30) / c->page_size || b->tokens > 0x7fffffff / c->kv_heads) return ATP_ERR_UNSUPPORTED;
     if (pointers) {
@@ -46,7 +48,7 @@ double moved_bytes(const atp_cache* c, const atp_batch* b, atp_dtype t) {
 }
 
 atp_status packed_shape(int64_t n_seq, int64_t tokens, int heads, int kv_heads, int d_h, const atp_dtype& t, ServeArgs& a) {
-    if (bad_dtype(t) || n_seq < 1 || n_seq > (1 << 24) || tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d_h < 1) return ATP_ERR_INVALID_ARG;
+    if (bad_dtype(t) || n_seq < 1 || n_seq > MAX_SEQ || tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d_h < 1) return ATP_ERR_INVALID_ARG;
     if (d_h % 8 || d_h > 256 || kv_heads > 65535 || tokens > 0x7fffffff / heads) return ATP_ERR_UNSUPPORTED;
     a.n_seq = (int)n_seq; a.tokens = (int)tokens; a.heads = heads; a.kv_heads = kv_heads; a.dh = d_h;
     a.max_kv = (int)tokens;

@@ -13,22 +13,16 @@ __device__ __forceinline__ float element(const T* p) {
     else return *p;
 }
 
-// One row over keys kt0 .. kt1-1, key after key, by a whole wave: features lane, lane + 64, ... with one pass of running maximum and sum.
-// No key that the row does not see is touched.
+// Sums of one row, held by a whole wave: features lane, lane + 64, ..., maximum of its scores and sum of its weights.
 struct RowSum { float o[4], m, l; };
 
+// Keys key0 .. key1-1 added to them, key after key.  No key that the row does not see is touched.
 template <typename T, int SRC>
-__device__ __forceinline__ RowSum attend_row(const ServeArgs& a, int seq, int first, int hk, const T* Qp, int key0, int key1) {
+__device__ __forceinline__ void attend_row(const ServeArgs& a, int seq, int first, int hk, const T* Qp, int key0, int key1, RowSum& r) {
     const int lane = threadIdx.x & 63;
     float qv[4];
-    RowSum r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        qv[i] = lane + 64 * i < a.dh ? element(Qp + lane + 64 * i) : 0.f;
-        r.o[i] = 0.f;
-    }
-    r.m = -INFINITY;
-    r.l = 0.f;
+    for (int i = 0; i < 4; ++i) qv[i] = lane + 64 * i < a.dh ? element(Qp + lane + 64 * i) : 0.f;
     for (int j = key0; j < key1; ++j) {
         float kv[4], vv[4];
         int64_t at = 0;
@@ -67,7 +61,6 @@ __device__ __forceinline__ RowSum attend_row(const ServeArgs& a, int seq, int fi
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.o[i] = fmaf(p, vv[i], r.o[i] * keep);
     }
-    return r;
 }
 
 template <typename T>
@@ -82,26 +75,49 @@ __device__ __forceinline__ void store_row(T* Op, const RowSum& r, int dh) {
         }
 }
 
-// The rows of an item, wave by wave, where a value that is not finite stands at a key that some of them do not see: a product of tiles
-// would carry it into every row (zero times infinity is NaN).
-template <typename T, int SRC, int ROWS_>
-__device__ __forceinline__ void attend_item_by_rows(const ServeArgs& a, const ServePlan& p, const ServeItem& it, int hk, int key0, int key1, int dp) {
+// Where a value that is not finite stands at a key that some rows of a tile do not see, the product of the tile would carry it into every row (zero
+// times infinity is NaN).  Such key tiles, bits of `bad` from tile kt0 on, are left out of the products; here they are added row by row to the
+// sums of 32 rows from row0 on, that lie in LDS (so: DP floats a row, sml: maximum and sum), and the rows are stored.  Only tiles that
+// hold the last keys of a row can be among them, so this is short however long the sequence is.
+template <typename T, int SRC, int DP, int KT_>
+__device__ __forceinline__ void finish_by_rows(const ServeArgs& a, const ServePlan& p, const ServeItem& it, int hk, int row0, const float* so, const float2* sml, unsigned bad,
+                                               int kt0) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned group = a.heads / a.kv_heads;
-    for (int row = it.row0 + wave; row < min(it.row0 + ROWS_, it.rows); row += 4) {
-        const int i = (int)((unsigned)row / group), h = hk * (int)group + (int)((unsigned)row % group);
-        const int keys = min(a.causal ? min(it.p0 + i + 1, it.kv) : it.kv, key1);
-        const RowSum r = attend_row<T, SRC>(a, it.seq, it.first, hk, reinterpret_cast<const T*>(a.Q) + (int64_t)(it.first + i) * a.ldq + (int64_t)h * a.dh, key0, keys);
+    for (int x = wave; x < 32 && row0 + x < it.rows; x += 4) {
+        const int row = row0 + x, i = (int)((unsigned)row / group), h = hk * (int)group + (int)((unsigned)row % group);
+        const int keys = a.causal ? min(it.p0 + i + 1, it.kv) : it.kv;
+        RowSum r;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) r.o[f] = lane + 64 * f < DP ? so[x * DP + lane + 64 * f] : 0.f;
+        r.m = sml[x].x;
+        r.l = sml[x].y;
+        for (unsigned left = bad; left; left &= left - 1) {
+            const int key0 = (kt0 + __builtin_ctz(left)) * KT_;
+            attend_row<T, SRC>(a, it.seq, it.first, hk, reinterpret_cast<const T*>(a.Q) + (int64_t)(it.first + i) * a.ldq + (int64_t)h * a.dh, key0, min(key0 + KT_, keys), r);
+        }
         if (it.nch == 1) {
             store_row(reinterpret_cast<T*>(a.O) + (int64_t)(it.first + i) * a.ldo + (int64_t)h * a.dh, r, a.dh);
         } else {
             const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
 #pragma unroll
             for (int f = 0; f < 4; ++f)
-                if (lane + 64 * f < dp) p.part_o[at * dp + lane + 64 * f] = r.o[f];
+                if (lane + 64 * f < DP) p.part_o[at * DP + lane + 64 * f] = r.o[f];
             if (lane == 0) p.part_ml[at] = make_float2(r.m, r.l);
         }
     }
+}
+
+// sums of a wave's 32 rows (a row to a lane, features 32i + 8g + 4·half .. +3 in registers 4g .. 4g+3 of o[i]) into LDS
+template <int DP, int NCT>
+__device__ __forceinline__ void sums_to_lds(const f32x16 (&o)[NCT], float m, float l, float* so, float2* sml) {
+    const int l32 = threadIdx.x & 31, lh = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int i = 0; i < NCT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4*>(so + l32 * DP + 32 * i + 8 * g + 4 * lh) = f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+    if (lh == 0) sml[l32] = make_float2(m, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -155,7 +171,8 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     __shared__ __align__(16) uint4 sK1[KT * CK];
     __shared__ __align__(16) uint4 sV0[KT * CK];
     __shared__ __align__(16) uint4 sV1[KT * CK];
-    __shared__ int sSpoilt;
+    __shared__ unsigned sBad;   // key tiles from kt_cross on that are left to finish_by_rows
+    __shared__ float2 sML[32];
 
     const int hk = blockIdx.x % a.kv_heads;   // consecutive workgroups go to the 8 XCDs in turn: a key head's items share an L2
     ServeItem it;
@@ -163,7 +180,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, lh = lane >> 5;
     const unsigned group = a.heads / a.kv_heads;
-    if (tid == 0) sSpoilt = 0;
+    if (tid == 0) sBad = 0;
 
     // last key that a row sees (negative: none); rows of a tile see more and more
     const auto last_key = [&](int row) { return a.causal ? min(it.p0 + (int)((unsigned)row / group), it.kv - 1) : it.kv - 1; };
@@ -176,6 +193,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
     // key tiles of this item
     const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
     const int kt_end = min((int)((int64_t)it.kt * (it.c + 1) / it.nch), (lim_tile1 + KT) / KT);
+    const int kt_cross = max(lim_tile0 + 1, 0) / KT;   // the first that some row does not see all of
 
     bf16x8 qf[NKS];
     {
@@ -385,13 +403,16 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
                 if (!((alive >> (c / CK)) & 1)) V[c] = make_uint4(0u, 0u, 0u, 0u);
             __syncthreads();
         }
+        bool bad = false;
         if (min(kt * KT + KT, it.kv) - 1 > lim_tile0) {   // some row does not see all keys: are their values finite?
             NotFinite n;
 #pragma unroll
             for (int i = 0; i < NL; ++i) n.take(V[i * 256 + tid]);
-            if (n.any()) sSpoilt = 1;
+            if (n.any()) atomicOr(&sBad, 1u << (kt - kt_cross));
+            __syncthreads();
+            bad = (sBad >> (kt - kt_cross)) & 1;
         }
-        if (kt * KT <= lim_wave1) compute(kt, K, V, alive);
+        if (kt * KT <= lim_wave1 && !bad) compute(kt, K, V, alive);
         pg0 = pg1;
         pg1 = pg2;
     };
@@ -408,12 +429,16 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
         if (kt + 1 < kt_end) step(kt + 1, sK1, sV1, true);
     }
     __syncthreads();
-    if (sSpoilt) {
-        attend_item_by_rows<bf16_t, SRC, ROWS>(a, p, it, hk, kt_begin * KT, kt_end * KT, DP);
+    const float l_tot = l_run + __shfl_xor(l_run, 32);
+    if (sBad) {
+        for (int w = 0; w < 4; ++w) {
+            if (wave == w) sums_to_lds<DP>(o, m_run, l_tot, reinterpret_cast<float*>(sK0), sML);
+            __syncthreads();
+            finish_by_rows<bf16_t, SRC, DP, KT>(a, p, it, hk, it.row0 + 32 * w, reinterpret_cast<const float*>(sK0), sML, sBad, kt_cross);
+            __syncthreads();
+        }
         return;
     }
-
-    const float l_tot = l_run + __shfl_xor(l_run, 32);
     if (it.nch > 1) {   // one of several chunks: sums as they are, with their maximum
         if (!live_row) return;
         const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
@@ -473,7 +498,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
     constexpr int NV = KT_S * LPR / 64;         // value loads of a lane
     __shared__ __align__(16) uint4 sV[4][KT_S * CK];
     __shared__ float2 sML[2][64];
-    __shared__ int sSpoilt;
+    __shared__ unsigned sBad;   // key tiles from kt_cross on that are left to finish_by_rows
 
     const int hk = blockIdx.x % a.kv_heads;
     ServeItem it;
@@ -489,7 +514,8 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
     const int lim0 = last_key(it.row0), lim1 = last_key(min(it.row0 + ROWS_S, it.rows) - 1);
     const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
     const int kt_end = min((int)((int64_t)it.kt * (it.c + 1) / it.nch), (lim1 + KT_S) / KT_S);
-    if (tid == 0) sSpoilt = 0;
+    const int kt_cross = max(lim0 + 1, 0) / KT_S;   // the first that some row does not see all of
+    if (tid == 0) sBad = 0;
     __syncthreads();
 
     // features of k-step ks that lane half lh multiplies: any order, as long as queries and keys agree
@@ -588,7 +614,6 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
 #pragma unroll
     for (int i = 0; i < NCT; ++i) v_col[i] = column_frag_offset<DP>(lane, 32 * i);
     const bool partial = lim0 < it.kv - 1;   // some row does not see all keys of the sequence
-    bool spoilt = false;
 
     int kt = kt_begin + wave;
     int pg0 = -1, pg1 = -1;
@@ -635,7 +660,12 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
             }
         }
         if (kt + 4 < kt_end) load_values(kt + 4, pg1);
-        if (min(kt * KT_S + KT_S, it.kv) - 1 > lim0 && seen.any()) spoilt = true;
+        if (min(kt * KT_S + KT_S, it.kv) - 1 > lim0 && __builtin_amdgcn_ballot_w64(seen.any()) != 0) {
+            if (lane == 0) atomicOr(&sBad, 1u << (kt - kt_cross));
+            pg0 = pg1;
+            pg1 = pg2;
+            continue;
+        }
         if (kt * KT_S + KT_S - 1 > lim0 || alive != ~0u) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
@@ -680,12 +710,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
         pg0 = pg1;
         pg1 = pg2;
     }
-    if (spoilt) sSpoilt = 1;
     __syncthreads();
-    if (sSpoilt) {
-        attend_item_by_rows<bf16_t, SRC, ROWS_S>(a, p, it, hk, kt_begin * KT_S, kt_end * KT_S, DP);
-        return;
-    }
     l_run += __shfl_xor(l_run, 32);
     // waves 2 and 3 hand their sums to waves 0 and 1, wave 1 to wave 0, at the larger maximum
     float* share = reinterpret_cast<float*>(sV);
@@ -712,6 +737,12 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
                 for (int v = 0; v < 16; ++v) o[i][v] = fmaf(share[wave * PER + (16 * i + v) * 64 + lane], f1, o[i][v] * f0);
         }
         __syncthreads();
+    }
+    if (sBad) {
+        if (wave == 0) sums_to_lds<DP>(o, m_run, l_run, share, sML[0]);
+        __syncthreads();
+        finish_by_rows<bf16_t, SRC, DP, KT_S>(a, p, it, hk, it.row0, share, sML[0], sBad, kt_cross);
+        return;
     }
     if (wave || !live_row) return;
     if (it.nch > 1) {
@@ -751,13 +782,14 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
     constexpr int NCT = DP / 32, NL = TK * DP / 4 / 256, RSTEP = 1024 / DP;
     __shared__ __align__(16) float sK[TK * PK];
     __shared__ __align__(16) float sV[TK * PV];
-    __shared__ int sSpoilt;
+    __shared__ unsigned sBad;   // key tiles from kt_cross on that are left to finish_by_rows
+    __shared__ float2 sML[32];
     const int hk = blockIdx.x % a.kv_heads;
     ServeItem it;
     if (!serve_item<ROWS_, TK>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
     const unsigned group = a.heads / a.kv_heads;
-    if (tid == 0) sSpoilt = 0;
+    if (tid == 0) sBad = 0;
     const auto last_key = [&](int row) { return a.causal ? min(it.p0 + (int)((unsigned)row / group), it.kv - 1) : it.kv - 1; };
     const int wrow0 = it.row0 + (KS == 1 ? 32 * wave : 0), row = wrow0 + l32;
     const bool live_row = row < it.rows;
@@ -766,6 +798,7 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
     const int lim_wave1 = wrow0 < it.rows ? last_key(min(wrow0 + 32, it.rows) - 1) : -1;
     const int kt_begin = (int)((int64_t)it.kt * it.c / it.nch);
     const int kt_end = min((int)((int64_t)it.kt * (it.c + 1) / it.nch), (lim_tile1 + TK) / TK);
+    const int kt_cross = max(lim_tile0 + 1, 0) / TK;   // the first that some row does not see all of
 
     const int qrow = min(row, it.rows - 1);   // rows past the end: any row, stored by nobody
     const int64_t token = it.first + (int)((unsigned)qrow / group), head = hk * (int)group + (int)((unsigned)qrow % group);
@@ -867,8 +900,9 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
                 for (int e = 0; e < 4; ++e) top += v[e] * 0.f;   // NaN as soon as one is infinite or NaN
             }
         }
-        if (partial && top != 0.f) sSpoilt = 1;
+        if (partial && top != 0.f) atomicOr(&sBad, 1u << (kt - kt_cross));
         __syncthreads();
+        const bool bad = partial && ((sBad >> (kt - kt_cross)) & 1);
         if constexpr (!PACKED) {
             pa = na; pb = nb;
             na = page_of(kt + 2, 0);
@@ -876,7 +910,7 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
         }
         if (kt + 1 < kt_end) load(kt + 1, pa, pb);
         const int kw = KS == 1 ? 0 : wave, key0 = kt * TK + 32 * kw;
-        if (key0 > lim_wave1) continue;
+        if (key0 > lim_wave1 || bad) continue;
         f32x16 s;
         // The matrix instruction adds one product after the other: sums of 16 features, added up, carry less of a rounding error than one chain.
         constexpr int NU = 2;   // k-groups of 8 in a sum
@@ -927,10 +961,6 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
         }
     }
     __syncthreads();
-    if (sSpoilt) {
-        attend_item_by_rows<float, SRC, ROWS_>(a, p, it, hk, kt_begin * TK, kt_end * TK, DP);
-        return;
-    }
     l_run += __shfl_xor(l_run, 32);
     if constexpr (KS > 1) {   // waves 2 and 3 hand their sums to waves 0 and 1, wave 1 to wave 0, at the larger maximum
         constexpr int PER = (NCT * 16 + 2) * 64;
@@ -960,9 +990,18 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
             }
             __syncthreads();
         }
-        if (wave) return;
     }
-    if (!live_row) return;
+    if (sBad) {
+#pragma unroll 1
+        for (int w = 0; w < 4 / KS; ++w) {
+            if (wave == w) sums_to_lds<DP>(o, m_run, l_run, sK, sML);
+            __syncthreads();
+            finish_by_rows<float, SRC, DP, TK>(a, p, it, hk, it.row0 + 32 * w, sK, sML, sBad, kt_cross);
+            __syncthreads();
+        }
+        return;
+    }
+    if ((KS > 1 && wave) || !live_row) return;
     const int64_t at = (int64_t)hk * p.part_rows + it.part + (int64_t)it.c * it.rows + row;
     const bool cut = it.nch > 1;   // one of several chunks: sums as they are, with their maximum
     if (cut && lh == 0) p.part_ml[at] = make_float2(m_run, l_run);

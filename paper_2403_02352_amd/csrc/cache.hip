@@ -23,6 +23,20 @@ __device__ __forceinline__ int row_exponent(float top) {
 
 struct Octet { float v[8]; };
 
+// eight elements as they lie in memory
+template <typename T>
+struct Raw {
+    uint4 u[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+    __device__ __forceinline__ void store(T* p, bool there) const {   // zeros where there are none
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(p)[i] = there ? u[i] : make_uint4(0, 0, 0, 0);
+    }
+};
+
 template <typename T>
 __device__ __forceinline__ Octet load8(const T* p) {
     Octet o;
@@ -74,10 +88,15 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a) {
         h[i] = !live[i] ? 0 : key[i] ? row : row - a.kv_heads;
         packed[i] = (int64_t)token * (key[i] ? a.ldk : a.ldv) + (int64_t)h[i] * a.dh + (live[i] ? piece * 8 : 0);
     }
-    Octet o[PER];
+    Octet o[PER];     // 8 bits: values; else rows are moved as they are
+    Raw<T> raw[PER];
     if constexpr (WRITE) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) o[i] = load8(reinterpret_cast<const T*>(key[i] ? a.Kn : a.Vn) + packed[i]);
+        for (int i = 0; i < PER; ++i) {
+            const T* p = reinterpret_cast<const T*>(key[i] ? a.Kn : a.Vn) + packed[i];
+            if constexpr (E4M3) o[i] = load8(p);
+            else raw[i].load(p);
+        }
     }
     const int s = sequence_of(a, token);
     if (s < 0) return;
@@ -114,7 +133,7 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a) {
                     if (piece == 0) (key[i] ? a.Ks : a.Vs)[at[i]] = (uint8_t)byte;
                 }
             } else if (live[i]) {
-                store8(reinterpret_cast<T*>(key[i] ? a.K : a.V) + at[i] * a.dh + piece * 8, o[i]);
+                raw[i].store(reinterpret_cast<T*>(key[i] ? a.K : a.V) + at[i] * a.dh + piece * 8, true);
             }
         }
     } else {
@@ -138,13 +157,18 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a) {
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) o[i] = load8(reinterpret_cast<const T*>(key[i] ? a.K : a.V) + at[i] * a.dh + f8);
+            for (int i = 0; i < PER; ++i) raw[i].load(reinterpret_cast<const T*>(key[i] ? a.K : a.V) + at[i] * a.dh + f8);
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
+            T* p = reinterpret_cast<T*>(key[i] ? a.Ko : a.Vo) + packed[i];
+            if constexpr (E4M3) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[i].v[e] = placed ? o[i].v[e] : 0.f;
-            if (live[i]) store8(reinterpret_cast<T*>(key[i] ? a.Ko : a.Vo) + packed[i], o[i]);
+                for (int e = 0; e < 8; ++e) o[i].v[e] = placed ? o[i].v[e] : 0.f;
+                if (live[i]) store8(p, o[i]);
+            } else if (live[i]) {
+                raw[i].store(p, placed);
+            }
         }
     }
 }

@@ -58,7 +58,7 @@ struct ServeItem {
 
 // Item w of a key head, the same for every thread of a wave; false behind the last.  Every wave finds it by itself from the lengths on the
 // device: the key tiles that all row tiles go through, over the number of items wanted, give the size of a chunk; then the sequences'
-// items are counted up, 64 sequences at a time.  The host knows none of the lengths, so calls can be captured, and the deal is even for
+// items are counted up, a sequence a lane, or a block of sequences a lane and then one a lane.  The host knows none of the lengths, so calls can be captured, and the deal is even for
 // any of them.  With `chunks` off, item w is row tile w.  Row tiles come in descending order: the last ones see the most keys.
 template <int ROWS, int KT>
 __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& p, int w, bool chunks, ServeItem& it) {
@@ -76,50 +76,73 @@ __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& 
     const auto key_tiles = [&] { return max((kv + KT - 1) / KT, 1); };
     const int steps = min(a.n_seq, 64);   // (lanes from n_seq on hold nothing: the exchanges stop there)
     const bool cut = p.part_rows > 0;
+    const int block = (a.n_seq + 63) / 64;   // sequences of a lane where there are more than lanes
     int chunk = 1 << 30;
     if (cut) {
         // (in floats, a little more than the share: the bound on the cuts holds whatever the sum's rounding)
         float total = 0.f;
-        for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-            look(s0 + lane);
+#pragma unroll 4
+        for (int i = 0; i < block; ++i) {
+            look(lane * block + i);
             total += (float)row_tiles() * (float)key_tiles();
         }
         for (int off = 1; off < steps; off <<= 1) total += __shfl_xor(total, off);
         const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(total)));
-        chunk = max((int)fminf(all * 1.00001f / (float)p.target + 1.f, 1e9f), p.min_chunk);
+        chunk = max((int)fminf(all * 1.0001f / (float)p.target + 1.f, 1e9f), p.min_chunk);
     }
-    int before = 0;
-    int64_t part = 0;
-    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        if (!cut || a.n_seq > 64) look(s0 + lane);
-        const int kt = key_tiles(), nch = (kt + chunk - 1) / chunk, rt = row_tiles();
-        const int mine = chunks ? rt * nch : rt;
-        const int mine_part = nch > 1 ? (int)min((int64_t)((unsigned)n * group) * nch, (int64_t)1 << 24) : 0;
-        int upto = mine, upto_part = mine_part;
+    int before = 0, part = 0, s0 = 0;
+    // items and partial rows of the sequence looked at last
+    const auto count = [&](int& items, int& rows) {
+        const int nch = (key_tiles() + chunk - 1) / chunk;
+        items = chunks ? row_tiles() * nch : row_tiles();
+        rows = nch > 1 ? (int)min((int64_t)((unsigned)n * group) * nch, (int64_t)1 << 22) : 0;
+    };
+    // sums over the lanes up to this one
+    const auto scan = [&](int v) {
         for (int off = 1; off < steps; off <<= 1) {
-            const int x = __shfl_up(upto, off);
-            if (lane >= off) upto += x;
+            const int x = __shfl_up(v, off);
+            if (lane >= off) v += x;
         }
-        if (cut)
-            for (int off = 1; off < steps; off <<= 1) {
-                const int y = __shfl_up(upto_part, off);
-                if (lane >= off) upto_part += y;
-            }
+        return v;
+    };
+    if (block > 1) {   // the lane whose sequences hold item w, then those sequences, one a lane
+        int mine = 0, mine_part = 0, items, rows;
+#pragma unroll 4
+        for (int i = 0; i < block; ++i) {
+            look(lane * block + i);
+            count(items, rows);
+            mine += items;
+            mine_part = min(mine_part + rows, 1 << 24);
+        }
+        const int upto = scan(mine), upto_part = scan(mine_part);
+        const unsigned long long behind = __builtin_amdgcn_ballot_w64(upto > w);
+        if (!behind) return false;
+        const int at = __builtin_ctzll(behind);
+        before = __builtin_amdgcn_readlane(upto - mine, at);
+        part = __builtin_amdgcn_readlane(upto_part - mine_part, at);
+        s0 = at * block;
+    }
+    const int s1 = min(s0 + block * (block > 1 ? 1 : 64), a.n_seq);
+    for (; s0 < s1; s0 += 64) {
+        if (!cut || block > 1) look(s0 + lane < s1 ? s0 + lane : a.n_seq);
+        int mine, mine_part;
+        count(mine, mine_part);
+        const int upto = scan(mine), upto_part = cut ? scan(mine_part) : 0;
         const unsigned long long behind = __builtin_amdgcn_ballot_w64(lane < steps && before + upto > w);
         if (behind) {
             const int at = __builtin_ctzll(behind);
             const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
             it.first = of(first); it.n = of(n); it.kv = of(kv); it.p0 = of(held) - it.n;
             it.rows = it.n * (int)group;
-            it.kt = of(kt);
+            it.kt = max((it.kv + KT - 1) / KT, 1);
             it.seq = s0 + at;
-            it.nch = of(nch);
+            it.nch = (it.kt + chunk - 1) / chunk;
             const int local = w - before - of(upto - mine), per = chunks ? it.nch : 1;
-            it.row0 = (of(rt) - 1 - local / per) * ROWS;
+            it.row0 = ((int)(((unsigned)it.rows + ROWS - 1) / ROWS) - 1 - local / per) * ROWS;
             it.c = local % per;
             it.part = part + of(upto_part - mine_part);
             // (offsets that decrease can count more rows than there are: no item for what the grid and the workspace do not hold)
-            return local >= 0 && local < of(mine) && (it.nch == 1 || it.part + (int64_t)it.rows * it.nch <= p.part_rows);
+            return local >= 0 && local < of(mine) && it.part >= 0 && (it.nch == 1 || it.part + (int64_t)it.rows * it.nch <= p.part_rows);
         }
         before += __builtin_amdgcn_readlane(upto, steps - 1);
         part += __builtin_amdgcn_readlane(upto_part, steps - 1);

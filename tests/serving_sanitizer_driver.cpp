@@ -61,7 +61,7 @@ int main() {
     EXPECT(bad_batch([](atp_batch& b) { b.length = nullptr; }) == ATP_ERR_INVALID_ARG);
     EXPECT(bad_batch([](atp_batch& b) { b.offsets = nullptr; }) == ATP_ERR_INVALID_ARG);
     EXPECT(bad_batch([&](atp_batch& b) { b.offsets = reinterpret_cast<const int32_t*>(P + 2); }) == ATP_ERR_INVALID_ARG);
-    for (int64_t n : {int64_t(0), int64_t(-3), INT64_MAX}) EXPECT(bad_batch([&](atp_batch& b) { b.n_seq = n; }) == ATP_ERR_INVALID_ARG);
+    for (int64_t n : {int64_t(0), int64_t(-3), int64_t(65537), INT64_MAX}) EXPECT(bad_batch([&](atp_batch& b) { b.n_seq = n; }) == ATP_ERR_INVALID_ARG);
     EXPECT(bad_batch([](atp_batch& b) { b.max_pages = 0; }) == ATP_ERR_INVALID_ARG);
     EXPECT(bad_batch([](atp_batch& b) { b.max_pages = INT64_MAX; }) == ATP_ERR_UNSUPPORTED);
     EXPECT(bad_batch([](atp_batch& b) { b.max_pages = (1 << 26) + 1; }) == ATP_ERR_UNSUPPORTED);
@@ -97,7 +97,7 @@ int main() {
     EXPECT(packed(P, P, 256, 128, I, 1, INT64_MAX, 4, 2, 64) == ATP_ERR_UNSUPPORTED);
 
     // workspace queries over sizes up to the limits: no overflow, and enough of it is asked for where it is asked for
-    for (int64_t n_seq : {1, 7, 300, 1 << 24}) for (int64_t tokens : {0, 1, 64, 5000, INT32_MAX / 256}) for (int d : {8, 64, 128, 256}) for (int hk : {1, 3, 32})
+    for (int64_t n_seq : {1, 7, 300, 65536}) for (int64_t tokens : {0, 1, 64, 5000, INT32_MAX / 256}) for (int d : {8, 64, 128, 256}) for (int hk : {1, 3, 32})
         for (int g : {1, 8}) for (int t = 0; t < 2; ++t) {
             EXPECT(atp_attention_packed_workspace(n_seq, tokens, hk * g, hk, d, (atp_dtype)t) % 256 == 0);
             for (int64_t pages : {int64_t(1), int64_t(4096), int64_t(1) << 26}) {

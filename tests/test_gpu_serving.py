@@ -530,6 +530,98 @@ def test_a_cache_beyond_32_bit_offsets(atp):
     check(got, *so.attention(host(Q), [host(K)], [host(V)], [0, 150], [150], True, 0.0), "bf16", 150)
 
 
+@pytest.mark.parametrize("dtype,kind", [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same")])
+def test_attention_paged_many_sequences_with_long_ones_among_them(atp, dtype, kind):
+    """More sequences than lanes, some of them empty, a few long enough to be cut."""
+    rng = np.random.default_rng(55)
+    for most_new in (1, 40):
+        lengths = rng.integers(0, 40, 150)
+        lengths[[3, 90, 149]] = [1500, 700, 1100]
+        new = np.minimum(lengths, rng.integers(0, most_new + 1, 150))
+        heads, hk, d = 4, 1, 64
+        p = Pages(atp, rng, lengths.tolist(), hk, d, 16, dtype, kind)
+        Q = randn(rng, (int(new.sum()), heads, d), dtype, 2.0)
+        offs = offsets_of(new)
+        K, V, present = p.gathered()
+        got = host(atp.attention_paged(Q, p.cache, ints(p.table), ints(lengths), ints(offs), max_new=most_new))
+        check(got, *so.attention(host(Q), K, V, offs, lengths, True, 0.0, present), dtype, 1500)
+
+
+def test_thousands_of_sequences(atp):
+    rng = np.random.default_rng(56)
+    n_seq, heads, hk, d = 5000, 2, 1, 64
+    lengths = rng.integers(0, 4, n_seq)
+    offs = offsets_of(lengths)
+    tokens = int(lengths.sum())
+    Q, K, V = (randn(rng, (tokens, h, d), "bf16") for h in (heads, hk, hk))
+    k, v = host(K), host(V)
+    cut = lambda x: [x[a:a + n] for a, n in so.bounds(offs, tokens)]  # noqa: E731
+    want = so.attention(host(Q), cut(k), cut(v), offs, lengths, True, 0.0)
+    check(host(atp.attention_packed(Q, K, V, ints(offs))), *want, "bf16", 4)
+    p = Pages(atp, rng, lengths.tolist(), hk, d, 1, "bf16", "same", fill=False)
+    atp.cache_write(p.cache, K, V, ints(p.table), ints(lengths), ints(offs))
+    check(host(atp.attention_paged(Q, p.cache, ints(p.table), ints(lengths), ints(offs))), *want, "bf16", 4)
+    back, _ = atp.cache_read(p.cache, ints(p.table), ints(lengths), ints(offs), tokens=tokens)
+    assert torch.equal(back, K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_that_make_no_sense_stay_within_the_tensors(atp, dtype):
+    """Decreasing and far offsets: nothing is read or written outside, whatever is computed."""
+    rng = np.random.default_rng(57)
+    heads, hk, d, tokens = 4, 2, 64, 64
+    p = Pages(atp, rng, [700, 64, 64, 64, 64, 64], hk, d, 16, dtype, "same")
+    wide = torch.full((tokens + 40, heads, d), 5.0, dtype=TORCH[dtype], device="cuda")
+    out = wide[20:20 + tokens]
+    Q, K, V = randn(rng, (tokens, heads, d), dtype), randn(rng, (tokens, hk, d), dtype), randn(rng, (tokens, hk, d), dtype)
+    for offs in ([0, 64, 0, 64, 0, 64, 0], [-5, 30, 10, 2 ** 31 - 1, -2 ** 31, 64, 64], [64, 0, 64, 0, 64, 0, 64]):
+        o = ints(offs)
+        args = (ints(p.table), ints([700, 64, 64, 64, 64, 64]), o)
+        atp.attention_packed(Q, K, V, o, out=out)
+        atp.attention_paged(Q, p.cache, *args, out=out)
+        atp.cache_read(p.cache, *args, out=(out[:, :hk], out[:, hk:]))
+        spare = sorted(set(range(p.n_pages)) - set(p.table.ravel().tolist()))
+        before = p.cache.K[spare].clone()
+        atp.cache_write(p.cache, K, V, *args)
+        torch.cuda.synchronize()
+        assert (wide[:20] == 5.0).all() and (wide[20 + tokens:] == 5.0).all() and torch.isfinite(wide).all()
+        assert torch.equal(p.cache.K[spare], before)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_the_same_type_are_moved_bit_by_bit(atp, dtype):
+    gen = torch.Generator("cuda").manual_seed(58)
+    as_int = torch.int16 if dtype == "bf16" else torch.int32
+    bits = torch.randint(-2 ** 15 if dtype == "bf16" else -2 ** 31, 2 ** 15 if dtype == "bf16" else 2 ** 31, (90, 6, 64), generator=gen, device="cuda", dtype=torch.int64).to(as_int)
+    x = bits.view(TORCH[dtype])
+    cache = atp.PagedCache.empty(6, 3, 16, 64, TORCH[dtype])
+    args = (ints([[5, 0, 3, 1, 4, 2]]), ints([90]), ints([0, 90]))
+    atp.cache_write(cache, x[:, :3], x[:, 3:], *args)
+    K, V = atp.cache_read(cache, *args, tokens=90)
+    assert torch.equal(K.view(as_int), bits[:, :3]) and torch.equal(V.view(as_int), bits[:, 3:])
+
+
+def test_values_that_are_not_finite_in_a_long_prompt_cost_no_more_than_their_tile(atp):
+    """A spoilt value far behind in a long prompt: the rows before it are as they should be, and the call stays quick."""
+    rng = np.random.default_rng(59)
+    n, heads, d = 6000, 2, 128
+    Q, K, V = (randn(rng, (n, heads, d), "bf16") for _ in range(3))
+    offs = ints([0, n])
+    clean = atp.attention_packed(Q, K, V, offs)
+    V[5500, :, 7] = float("inf")
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    atp.attention_packed(Q, K, V, offs)
+    start.record()
+    got = atp.attention_packed(Q, K, V, offs)
+    end.record()
+    torch.cuda.synchronize()
+    same = (got[:5400] == clean[:5400]).all() and torch.isfinite(got[:5500]).all() and not torch.isfinite(got[5500:, :, 7]).any()
+    assert same
+    rest = torch.arange(d, device="cuda") != 7
+    assert (got[..., rest].float() - clean[..., rest].float()).abs().max() <= 2 ** -7 * clean.float().abs().max()
+    assert start.elapsed_time(end) < 20.0
+
+
 # ------------------------------------------------------------------ refusals of the binding
 def test_refusals(atp):
     bf = torch.bfloat16
