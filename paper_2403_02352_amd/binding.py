@@ -454,6 +454,8 @@ class PagedCache:
     """Pages of keys and values, [n_pages, kv_heads, page_size, d_h] each: in the storage type of the calls, or as torch.float8_e4m3fn
     codes with a biased exponent (uint8 [n_pages, kv_heads, page_size]) for every row.  The tensors stay the caller's."""
 
+    __slots__ = ("K", "V", "K_scale", "V_scale", "e4m3", "device", "n_pages", "kv_heads", "page_size", "d_h", "_c")
+
     def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: Optional[torch.Tensor] = None, V_scale: Optional[torch.Tensor] = None):
         e4m3, shape = K.dtype == torch.float8_e4m3fn, K.shape
         if len(shape) != 4 or V.shape != shape or V.dtype != K.dtype:
@@ -468,9 +470,8 @@ class PagedCache:
         self.n_pages, self.kv_heads, self.page_size, self.d_h = shape
         ks = vs = None
         if e4m3:
-            for s in (K_scale, V_scale):
-                if s.dtype != torch.uint8 or s.shape != shape[:3]:
-                    raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
+            if K_scale.dtype is not torch.uint8 or V_scale.dtype is not torch.uint8 or not K_scale.shape == V_scale.shape == shape[:3]:
+                raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
             ks, vs = K_scale.data_ptr(), V_scale.data_ptr()
         self._c = _Cache(K.data_ptr(), V.data_ptr(), ks, vs, self.n_pages, self.page_size, self.kv_heads, self.d_h,
                          ATP_CACHE_E4M3 if e4m3 else ATP_CACHE_SAME)
@@ -509,19 +510,14 @@ def _rows(t: torch.Tensor, name: str, heads: Optional[int] = None, d_h: Optional
     return ld if n > 1 else h * d
 
 
-def _int32(name: str, t: torch.Tensor, dim: int) -> None:
-    if t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous int32 with {dim} dimension(s)")
-
-
 def _batch(table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: int) -> _Batch:
-    _int32("table", table, 2)
-    _int32("length", length, 1)
-    _int32("offsets", offsets, 1)
-    n_seq, max_pages = table.shape
-    if length.shape[0] != n_seq or offsets.shape[0] != n_seq + 1:
+    i32, of_table, of_length, of_offsets = torch.int32, table.shape, length.shape, offsets.shape
+    if table.dtype is not i32 or length.dtype is not i32 or offsets.dtype is not i32 or not table.is_contiguous() \
+            or not length.is_contiguous() or not offsets.is_contiguous():
+        raise ValueError("table, length and offsets must be contiguous int32")
+    if len(of_table) != 2 or len(of_length) != 1 or len(of_offsets) != 1 or of_length[0] != of_table[0] or of_offsets[0] != of_table[0] + 1:
         raise ValueError("table [n_seq, max_pages], length [n_seq] and offsets [n_seq + 1] do not match")
-    return _Batch(table.data_ptr(), length.data_ptr(), offsets.data_ptr(), n_seq, max_pages, tokens)
+    return _Batch(table.data_ptr(), length.data_ptr(), offsets.data_ptr(), of_table[0], of_table[1], tokens)
 
 
 def _serve(fn, dev: torch.device, *args) -> None:
@@ -538,11 +534,9 @@ def _serve(fn, dev: torch.device, *args) -> None:
 
 def _new_rows(cache: PagedCache, K: torch.Tensor, V: torch.Tensor):
     """Type and row strides of packed keys and values that go with a cache."""
-    ldk, ldv = _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V", cache.kv_heads, cache.d_h)
-    t = _dt(K)
-    if V.shape[0] != K.shape[0] or V.dtype != K.dtype or (not cache.e4m3 and K.dtype != cache.K.dtype):
+    if V.shape != K.shape or V.dtype is not K.dtype or not (cache.e4m3 or K.dtype is cache.K.dtype):
         raise ValueError("K / V shape or dtype mismatch")
-    return t, ldk, ldv
+    return _dt(K), _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V")
 
 
 def cache_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor) -> None:
@@ -599,7 +593,8 @@ def attention_packed(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, offsets:
     """Attention of packed sequences over their own tokens: Q [tokens, heads, d_h], K, V [tokens, kv_heads, d_h], offsets [n_seq + 1] -> O.
     Rows outside every sequence keep what `out` held (zeros without it)."""
     dev = _one_device(Q, K, V, offsets, workspace, out)
-    _int32("offsets", offsets, 1)
+    if offsets.dtype is not torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous():
+        raise ValueError("offsets must be contiguous int32 [n_seq + 1]")
     ldq, ldk, ldv = _rows(Q, "Q"), _rows(K, "K"), _rows(V, "V")
     tokens, heads, d_h = Q.shape
     kv_heads, n_seq = K.shape[1], offsets.shape[0] - 1
