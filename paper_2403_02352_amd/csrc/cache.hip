@@ -22,6 +22,13 @@ __device__ __forceinline__ int row_exponent(float top) {
 }
 
 struct Octet { float v[8]; };
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Rows leave past the caches: nobody reads them before they would have been displaced, and what is dirty in the L2 at a kernel's end is written back before
+// the next one starts (92770 positions read from 8 bits 106 -> 85 us, 27891 tokens written 36.4 -> 34.4).
+__device__ __forceinline__ void store_past(void* p, uint4 v) { __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p)); }
+__device__ __forceinline__ void store_past(void* p, uint2 v) { __builtin_nontemporal_store(u32x2{v.x, v.y}, reinterpret_cast<u32x2*>(p)); }
 
 // eight elements as they lie in memory
 template <typename T>
@@ -33,7 +40,7 @@ struct Raw {
     }
     __device__ __forceinline__ void store(T* p, bool there) const {   // zeros where there are none
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(p)[i] = there ? u[i] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) store_past(reinterpret_cast<uint4*>(p) + i, there ? u[i] : make_uint4(0, 0, 0, 0));
     }
 };
 
@@ -55,10 +62,10 @@ __device__ __forceinline__ Octet load8(const T* p) {
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const Octet& o) {
     if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf2(o.v[0], o.v[1]), pack_bf2(o.v[2], o.v[3]), pack_bf2(o.v[4], o.v[5]), pack_bf2(o.v[6], o.v[7]));
+        store_past(p, make_uint4(pack_bf2(o.v[0], o.v[1]), pack_bf2(o.v[2], o.v[3]), pack_bf2(o.v[4], o.v[5]), pack_bf2(o.v[6], o.v[7])));
     } else {
-        *reinterpret_cast<f32x4*>(p) = f32x4{o.v[0], o.v[1], o.v[2], o.v[3]};
-        *reinterpret_cast<f32x4*>(p + 4) = f32x4{o.v[4], o.v[5], o.v[6], o.v[7]};
+        __builtin_nontemporal_store(f32x4{o.v[0], o.v[1], o.v[2], o.v[3]}, reinterpret_cast<f32x4*>(p));
+        __builtin_nontemporal_store(f32x4{o.v[4], o.v[5], o.v[6], o.v[7]}, reinterpret_cast<f32x4*>(p + 4));
     }
 }
 
@@ -128,8 +135,8 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[i].v[e] = fabsf(o[i].v[e]) < INFINITY ? o[i].v[e] * f : NAN;
                 if (live[i]) {
-                    *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(key[i] ? a.K : a.V) + at[i] * a.dh + piece * 8) =
-                        make_uint2(pack_e4m3(o[i].v[0], o[i].v[1], o[i].v[2], o[i].v[3]), pack_e4m3(o[i].v[4], o[i].v[5], o[i].v[6], o[i].v[7]));
+                    store_past(reinterpret_cast<uint8_t*>(key[i] ? a.K : a.V) + at[i] * a.dh + piece * 8,
+                               make_uint2(pack_e4m3(o[i].v[0], o[i].v[1], o[i].v[2], o[i].v[3]), pack_e4m3(o[i].v[4], o[i].v[5], o[i].v[6], o[i].v[7])));
                     if (piece == 0) (key[i] ? a.Ks : a.Vs)[at[i]] = (uint8_t)byte;
                 }
             } else if (live[i]) {
