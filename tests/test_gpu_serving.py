@@ -622,6 +622,77 @@ def test_values_that_are_not_finite_in_a_long_prompt_cost_no_more_than_their_til
     assert start.elapsed_time(end) < 20.0
 
 
+WIDTHS = [
+    # lengths, new tokens, heads, kv_heads, d_h, page size: widths that are no multiple of 16, many heads to a key head, wide tables
+    ([300, 20], [1, 1], 128, 1, 72, 32),
+    ([300, 20], [150, 3], 4, 2, 104, 64),
+    ([150, 90], [40, 90], 2, 1, 200, 16),
+    ([260], [7], 96, 2, 24, 128),
+    ([1200, 70], [1, 1], 16, 2, 200, 64),
+]
+
+
+@pytest.mark.parametrize("dtype,kind", [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same"), ("f32", "e4m3")])
+@pytest.mark.parametrize("case", WIDTHS, ids=str)
+def test_attention_of_odd_widths_with_a_scale_of_its_own_into_column_blocks(atp, dtype, kind, case):
+    lengths, new, heads, hk, d, page = case
+    rng = np.random.default_rng(61)
+    p = Pages(atp, rng, lengths, hk, d, page, dtype, kind, most=-(-max(lengths) // page) + 5)
+    for s, n in enumerate(lengths):   # what stands behind a sequence's pages is not looked at
+        p.table[s, -(-n // page):] = rng.choice([-1, 0, 2 ** 31 - 1, -2 ** 31])
+    offs = offsets_of(new)
+    Q = randn(rng, (sum(new), heads, d), dtype, 2.0)
+    K, V, present = p.gathered()
+    wide = torch.full((sum(new), heads + 3, d), 9.0, dtype=TORCH[dtype], device="cuda")
+    for scale in (0.02, 1.0):
+        got = atp.attention_paged(Q, p.cache, ints(p.table), ints(lengths), ints(offs), scale=scale, out=wide[:, 2:2 + heads])
+        check(host(got), *so.attention(host(Q), K, V, offs, lengths, True, scale, present), dtype, max(lengths))
+        assert (wide[:, :2] == 9.0).all() and (wide[:, 2 + heads:] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [24, 72, 104, 200])
+def test_attention_packed_of_odd_widths(atp, dtype, d):
+    rng = np.random.default_rng(62)
+    for lengths, heads, hk in (([150, 7], 6, 2), ([20, 1, 9], 64, 1)):
+        tokens, offs = sum(lengths), offsets_of(lengths)
+        Q, K, V = (randn(rng, (tokens, h, d), dtype, 1.5) for h in (heads, hk, hk))
+        wide = torch.full((tokens, heads + 1, d), 9.0, dtype=TORCH[dtype], device="cuda")
+        got = host(atp.attention_packed(Q, K, V, ints(offs), scale=0.1, out=wide[:, 1:]))
+        k, v = host(K), host(V)
+        cut = lambda x: [x[a:a + n] for a, n in so.bounds(offs, tokens)]  # noqa: E731
+        check(got, *so.attention(host(Q), cut(k), cut(v), offs, lengths, True, 0.1), dtype, max(lengths))
+        assert (wide[:, 0] == 9.0).all()
+
+
+def test_two_captured_calls_share_a_workspace(atp):
+    """Two graphs over one workspace, replayed in turn with eager work between them, give what eager calls give."""
+    rng = np.random.default_rng(63)
+    p = Pages(atp, rng, [3000, 500], 2, 64, 64, "bf16", "e4m3")
+    table, length, offs = ints(p.table), ints([3000, 500]), ints([0, 1, 2])
+    Q = [randn(rng, (2, 8, 64), "bf16") for _ in range(2)]
+    ws = torch.empty(atp.attention_paged_workspace(p.cache, 2, table.shape[1], 2, 8, torch.bfloat16, 1), dtype=torch.uint8, device="cuda")
+    out = [torch.zeros_like(q) for q in Q]
+    call = lambda i: atp.attention_paged(Q[i], p.cache, table, length, offs, max_new=1, workspace=ws, out=out[i])  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(0)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(i)
+    for _ in range(3):
+        for i in range(2):
+            Q[i].copy_(randn(rng, Q[i].shape, "bf16"))
+            ws.fill_(255)   # what the workspace held does not matter
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[i], atp.attention_paged(Q[i], p.cache, table, length, offs, max_new=1))
+
+
 # ------------------------------------------------------------------ refusals of the binding
 def test_refusals(atp):
     bf = torch.bfloat16
