@@ -1060,7 +1060,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(ServeArgs a, ServePlan p
         if (c0 + l32 < it.nch) {
             const float2 ml = p.part_ml[at + (int64_t)(c0 + l32) * it.rows];
             w = __builtin_amdgcn_exp2f((ml.x - ref) * c_log2e);
-            lw = w == 0.f ? 0.f : ml.y * w;
+            lw = ml.y * w;   // (NaN stays NaN, also at a weight of zero)
         }
         const int n = min(32, it.nch - c0);
         for (int c = 0; c < n; c += 8) {
@@ -1069,10 +1069,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(ServeArgs a, ServePlan p
             for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const Share*>(p.part_o + (at + (int64_t)(c0 + min(c + k, n - 1)) * it.rows) * DP + NF * l32);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float wk = __shfl(w, c + k, 32);   // (zero behind the last chunk)
+                const float wk = __shfl(w, c + k, 32);
                 l += __shfl(lw, c + k, 32);
 #pragma unroll
-                for (int e = 0; e < NF; ++e) o[e] = wk == 0.f ? o[e] : fmaf(v[k][e], wk, o[e]);
+                for (int e = 0; e < NF; ++e) o[e] = c + k < n ? fmaf(v[k][e], wk, o[e]) : o[e];
             }
         }
     }

@@ -693,6 +693,28 @@ def test_two_captured_calls_share_a_workspace(atp):
             assert torch.equal(out[i], atp.attention_paged(Q[i], p.cache, table, length, offs, max_new=1))
 
 
+@pytest.mark.parametrize("dtype,kind", [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same"), ("f32", "e4m3")])
+@pytest.mark.parametrize("what", ["K", "V"])
+def test_values_that_are_nan_reach_the_sum_from_a_part_of_the_keys_that_weighs_nothing(atp, dtype, kind, what):
+    """Key 4000 outweighs every other by more than the exponents of 32 bits; a NaN at key 100, in another share of the keys, still makes NaN: of
+    every feature when it stands in the key, of its own feature in the value."""
+    rng = np.random.default_rng(31)
+    n, heads, d, page = 4096, 2, 64, 64
+    K, V, Q = randn(rng, (n, 1, d), dtype), randn(rng, (n, 1, d), dtype), randn(rng, (1, heads, d), dtype)
+    Q[:, :, 0], K[:, :, 0], K[4000, :, 0] = 40.0, 0.0, 400.0
+    (K if what == "K" else V)[100, 0, 5] = float("nan")
+    cache = atp.PagedCache.empty(n // page, 1, page, d, torch.float8_e4m3fn if kind == "e4m3" else TORCH[dtype])
+    table = ints(np.arange(n // page)[None])
+    atp.cache_write(cache, K, V, table, ints([n]), ints([0, n]))
+    print(f"nan {dtype} {kind} {what}", flush=True)
+    got = host(atp.attention_paged(Q, cache, table, ints([n]), ints([0, 1])))
+    nan = np.ones(d, bool) if what == "K" else np.arange(d) == 5
+    assert np.array_equal(np.isnan(got), np.broadcast_to(nan, got.shape))
+    code = host(V[4000, 0]) if kind == "same" else host(atp.cache_read(cache, table, ints([4001]), ints([0, 1]), tokens=1, dtype=torch.float32)[1][0, 0])
+    if what == "V":
+        assert np.abs(got - code)[..., ~nan].max() <= HALF[dtype] * 4 * np.abs(code).max()
+
+
 # ------------------------------------------------------------------ refusals of the binding
 def test_refusals(atp):
     bf = torch.bfloat16
