@@ -389,7 +389,7 @@ atp_status atp_norm_factored(const void* P, const void* C, const float* gain, fl
  * Tokens of several sequences lie one behind the other in [tokens, heads, d_h] tensors; `offsets` [n_seq + 1] (device int32) says where
  * each sequence starts: tokens offsets[s] … offsets[s+1] − 1 belong to sequence s (none when both are equal).  Rows outside every sequence
  * are not written, and what they hold reaches nobody.  A token's row of heads·d_h elements is contiguous, rows are a stride (ldq, ldk, ldv, ldo, in elements)
- * apart, so Q, K and V may be column blocks of one packed projection.  Every stride is a multiple of 16 bytes and at least the row.
+ * apart, so Q, K and V may be column blocks of one packed projection.  Every stride is a multiple of 16 bytes, at least the row and at most 2^24 elements.
  * At most 65536 sequences a call.  `heads` is a multiple of `kv_heads`: query head h reads key head h / (heads / kv_heads).  d_h is a multiple of 8 up to 256.
  * Offsets are read on the device only: they may change between replays of a captured graph, as long as `tokens` and `n_seq` stay.
  * Values outside 0 … tokens are taken to the nearest bound, a sequence that ends before it starts is empty, and the sequences of offsets
@@ -428,7 +428,8 @@ typedef struct {
 
 /* Rows of the new tokens into their places in the cache.  K, V [tokens, kv_heads, d_h] (type t).  Two tokens with one place (a page that
  * two sequences share and both write) leave one of their rows there, whole or mixed.
- * Errors: ATP_ERR_INVALID_ARG (null, misaligned, bad size, stride or enum), ATP_ERR_DEVICE. */
+ * Errors: ATP_ERR_INVALID_ARG (null, misaligned, bad size, stride or enum), ATP_ERR_UNSUPPORTED (d_h above 256 or no multiple of 8; more
+ * than 65535 key heads; tokens·kv_heads >= 2^31; max_pages·page_size > 2^30), ATP_ERR_DEVICE. */
 atp_status atp_cache_write(const atp_cache* cache, const atp_batch* batch, const void* K, const void* V, int64_t ldk, int64_t ldv,
                            atp_dtype t, void* hip_stream);
 
@@ -440,9 +441,9 @@ atp_status atp_cache_read(const atp_cache* cache, const atp_batch* batch, void* 
  *     O[i, h] = Σ_j softmax_j(scale · <Q[i, h], K[j, h / (heads/kv_heads)]>) · V[j, h / (heads/kv_heads)],
  * j over the tokens of the sequence, with `causal` (not 0) those up to i.  scale <= 0: 1/sqrt(d_h).  Values of keys that a query does not
  * see never reach it, also when they are not finite.  A query all of whose scores are −inf gives zeros.
- * Workspace: 0 bytes for some shapes; depends on sizes only.
- * Errors: ATP_ERR_INVALID_ARG, ATP_ERR_UNSUPPORTED (d_h above 256 or no multiple of 8; tokens·heads >= 2^31), ATP_ERR_WORKSPACE,
- * ATP_ERR_DEVICE. */
+ * Workspace: 0 bytes for some shapes; depends on sizes only.  Scratch of one call: calls that share it must not overlap in time.
+ * Errors: ATP_ERR_INVALID_ARG, ATP_ERR_UNSUPPORTED (d_h above 256 or no multiple of 8; more than 65535 key heads; tokens·heads >= 2^31),
+ * ATP_ERR_WORKSPACE, ATP_ERR_DEVICE. */
 size_t atp_attention_packed_workspace(int64_t n_seq, int64_t tokens, int heads, int kv_heads, int d_h, atp_dtype t);
 
 atp_status atp_attention_packed(const void* Q, const void* K, const void* V, void* O, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo,

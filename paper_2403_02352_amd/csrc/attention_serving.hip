@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
 
     const int hk = blockIdx.x % a.kv_heads;   // consecutive workgroups go to the 8 XCDs in turn: a key head's items share an L2
     ServeItem it;
-    if (!serve_item<ROWS, KT>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
+    if (!serve_item<ROWS, KT>(a, p, blockIdx.x / a.kv_heads + blockIdx.y * p.per_row, true, it)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, lh = lane >> 5;
     const unsigned group = a.heads / a.kv_heads;
@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
 
     const int hk = blockIdx.x % a.kv_heads;
     ServeItem it;
-    if (!serve_item<ROWS_S, KT_S>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
+    if (!serve_item<ROWS_S, KT_S>(a, p, blockIdx.x / a.kv_heads + blockIdx.y * p.per_row, true, it)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, lh = lane >> 5;
     const unsigned group = a.heads / a.kv_heads;
@@ -800,7 +800,7 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
     __shared__ float2 sML[32];
     const int hk = blockIdx.x % a.kv_heads;
     ServeItem it;
-    if (!serve_item<ROWS_, TK>(a, p, blockIdx.x / a.kv_heads, true, it)) return;
+    if (!serve_item<ROWS_, TK>(a, p, blockIdx.x / a.kv_heads + blockIdx.y * p.per_row, true, it)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
     const unsigned group = a.heads / a.kv_heads;
     if (tid == 0) sBad = 0;
@@ -1127,15 +1127,19 @@ ServePlan plan_f32(const ServeArgs& a, bool few) { return few ? plan_of(a, 32, 1
 
 size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
 
+// A workgroup for every item of every key head, in rows of at most 2^22 workgroups: a launch takes fewer than 2^32 threads along x.
+dim3 grid_of(const ServeArgs& a, ServePlan& p) {
+    p.per_row = std::min(p.items, (1 << 22) / a.kv_heads);
+    return dim3((unsigned)(p.per_row * a.kv_heads), (unsigned)((p.items + p.per_row - 1) / p.per_row));
+}
+
 template <int DP>
 hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool few, void* workspace) {
     ServePlan p = plan_bf16(a, few);
     p.part_o = reinterpret_cast<float*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.part_rows * a.kv_heads * DP);
     const float c = a.scale * 1.4426950408889634f;
-    const int64_t blocks = (int64_t)p.items * a.kv_heads;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid = grid_of(a, p);
     const bool full = a.dh == DP;
     if (few) {
         const bool whole = a.page_shift >= 5;
@@ -1177,9 +1181,7 @@ template <int DP, int KS>
 hipError_t launch_f32(hipStream_t st, const ServeArgs& a, KvSource src, ServePlan p, void* workspace) {
     p.part_o = reinterpret_cast<float*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.part_rows * a.kv_heads * DP);
-    const int64_t blocks = (int64_t)p.items * a.kv_heads;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid = grid_of(a, p);
     if (src == KV_PACKED) hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PACKED>), grid, dim3(256), 0, st, a, p);
     else if (src == KV_PAGED) hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PAGED>), grid, dim3(256), 0, st, a, p);
     else hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a, p);

@@ -1,6 +1,8 @@
 // Writing the rows of new tokens into the pages of a cache and reading them back, as they are or as 8-bit floats with a power of two per row.
 #include "serving.h"
 
+#include <algorithm>
+
 namespace atp {
 namespace {
 
@@ -74,15 +76,16 @@ __device__ __forceinline__ void store8(T* p, const Octet& o) {
 // on their way: where they come from depends on nothing else.
 // Bound by memory for prompts (each element read once and written once), by the chain offsets - table - row for the tokens of a step.
 constexpr int PER = 4;
+constexpr int64_t GRID_ROW = 1 << 22;   // workgroups of a row of the grid: a launch takes fewer than 2^32 threads along x
 
 template <typename T, bool E4M3, bool WRITE, int GS>
 __global__ void __launch_bounds__(256) cache_rows_kernel(ServeArgs a) {
     constexpr int RPW = 64 >> GS;                                    // rows of a wave-ful
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t w = (blockIdx.y * GRID_ROW + blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int slices = (2 * a.kv_heads + PER * RPW - 1) / (PER * RPW);
+    if (w >= (int64_t)a.tokens * slices) return;
     const int token = __builtin_amdgcn_readfirstlane((int)(w / slices)), slice = __builtin_amdgcn_readfirstlane((int)(w % slices));
-    if (token >= a.tokens) return;
     const int piece = lane & ((1 << GS) - 1);
     bool live[PER], key[PER];
     int h[PER];
@@ -185,8 +188,7 @@ hipError_t launch_group(hipStream_t st, const ServeArgs& a, int elem_bytes, bool
     constexpr int RPW = 64 >> GS;
     const int64_t slices = (2 * (int64_t)a.kv_heads + PER * RPW - 1) / (PER * RPW);
     const int64_t blocks = ((int64_t)a.tokens * slices + 3) / 4;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)std::min(blocks, GRID_ROW), (unsigned)((blocks + GRID_ROW - 1) / GRID_ROW));
     if (elem_bytes == 2) {
         if (e4m3) hipLaunchKernelGGL((cache_rows_kernel<bf16_t, true, WRITE, GS>), grid, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((cache_rows_kernel<bf16_t, false, WRITE, GS>), grid, dim3(256), 0, st, a);

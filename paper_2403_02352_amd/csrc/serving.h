@@ -34,6 +34,7 @@ hipError_t cache_read_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, b
 struct ServePlan {
     int target = 1, min_chunk = 1;
     int tiles = 0, items = 0;   // bounds of the row tiles and of the items of a key head
+    int per_row = 1;            // items of a key head that a row of the grid holds
     int64_t part_rows = 0;      // bound of the partial rows of a key head
     float* part_o = nullptr;
     float2* part_ml = nullptr;

@@ -715,6 +715,32 @@ def test_values_that_are_nan_reach_the_sum_from_a_part_of_the_keys_that_weighs_n
         assert np.abs(got - code)[..., ~nan].max() <= HALF[dtype] * 4 * np.abs(code).max()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_workgroups_than_a_row_of_the_grid_holds(atp, dtype):
+    """512 sequences of one token, 32768 heads: more than 2^24 workgroups.  A single key weighs 1, so every head gives its value."""
+    n, heads, d = 512, 32768, 8
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    Q, K, V = (torch.randn((n, heads, d), dtype=TORCH[dtype], device="cuda", generator=gen) for _ in range(3))
+    print(f"workgroups {dtype}", flush=True)
+    assert torch.equal(atp.attention_packed(Q, K, V, ints(np.arange(n + 1))), V)
+
+
+def test_more_tokens_than_a_row_of_the_grid_holds(atp):
+    """2^26 + 1000 tokens of one head: written and read bit by bit."""
+    n, page = 2 ** 26 + 1000, 65536
+    pages = (n + page - 1) // page
+    print("tokens", flush=True)
+    bits = torch.arange(n * 4, dtype=torch.int32, device="cuda")
+    K, V = bits.view(torch.bfloat16).view(n, 1, 8), (bits ^ 0x55555555).view(torch.bfloat16).view(n, 1, 8)
+    cache = atp.PagedCache.empty(pages, 1, page, 8, torch.bfloat16)
+    table = ints(np.random.default_rng(6).permutation(pages)[None])
+    out = torch.zeros_like(K), torch.zeros_like(V)
+    atp.cache_write(cache, K, V, table, ints([n]), ints([0, n]))
+    atp.cache_read(cache, table, ints([n]), ints([0, n]), out=out)
+    as_bits = lambda t: t.view(-1).view(torch.int32)  # noqa: E731
+    assert torch.equal(as_bits(out[0]), as_bits(K)) and torch.equal(as_bits(out[1]), as_bits(V))
+
+
 # ------------------------------------------------------------------ refusals of the binding
 def test_refusals(atp):
     bf = torch.bfloat16
