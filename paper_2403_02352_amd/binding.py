@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from operator import attrgetter
 from typing import Optional
 
 import torch
@@ -452,9 +453,12 @@ ATP_CACHE_SAME, ATP_CACHE_E4M3 = 0, 1
 
 class PagedCache:
     """Pages of keys and values, [n_pages, kv_heads, page_size, d_h] each: in the storage type of the calls, or as torch.float8_e4m3fn
-    codes with a biased exponent (uint8 [n_pages, kv_heads, page_size]) for every row.  The tensors stay the caller's."""
+    codes with a biased exponent (uint8 [n_pages, kv_heads, page_size]) for every row.  The tensors stay the caller's; the object holds their
+    addresses, so its attributes are read-only and a call with a tensor that has moved since (resize_, set_) is refused: a cache that
+    grows is a new object."""
 
-    __slots__ = ("K", "V", "K_scale", "V_scale", "e4m3", "device", "n_pages", "kv_heads", "page_size", "d_h", "_c")
+    _NAMES = ("K", "V", "K_scale", "V_scale", "e4m3", "device", "n_pages", "kv_heads", "page_size", "d_h")
+    __slots__ = tuple("_" + n for n in _NAMES) + ("_c", "_at")
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: Optional[torch.Tensor] = None, V_scale: Optional[torch.Tensor] = None):
         e4m3, shape = K.dtype == torch.float8_e4m3fn, K.shape
@@ -464,17 +468,21 @@ class PagedCache:
             _dt(K)
         if (K_scale is not None) != e4m3 or (V_scale is not None) != e4m3:
             raise ValueError("float8_e4m3fn pages have scales, others none")
-        self.device = _one_device(K, V, K_scale, V_scale)
+        self._device = _one_device(K, V, K_scale, V_scale)
         _check(K, V, K_scale, V_scale)
-        self.K, self.V, self.K_scale, self.V_scale, self.e4m3 = K, V, K_scale, V_scale, e4m3
-        self.n_pages, self.kv_heads, self.page_size, self.d_h = shape
-        ks = vs = None
-        if e4m3:
-            if K_scale.dtype is not torch.uint8 or V_scale.dtype is not torch.uint8 or not K_scale.shape == V_scale.shape == shape[:3]:
-                raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
-            ks, vs = K_scale.data_ptr(), V_scale.data_ptr()
-        self._c = _Cache(K.data_ptr(), V.data_ptr(), ks, vs, self.n_pages, self.page_size, self.kv_heads, self.d_h,
-                         ATP_CACHE_E4M3 if e4m3 else ATP_CACHE_SAME)
+        self._K, self._V, self._K_scale, self._V_scale, self._e4m3 = K, V, K_scale, V_scale, e4m3
+        self._n_pages, self._kv_heads, self._page_size, self._d_h = n_pages, kv_heads, page_size, d_h = shape
+        if e4m3 and (K_scale.dtype is not torch.uint8 or V_scale.dtype is not torch.uint8 or not K_scale.shape == V_scale.shape == shape[:3]):
+            raise ValueError("scales must be uint8 [n_pages, kv_heads, page_size]")
+        self._at = k, v, ks, vs = K.data_ptr(), V.data_ptr(), K_scale.data_ptr() if e4m3 else None, V_scale.data_ptr() if e4m3 else None
+        self._c = _Cache(k, v, ks, vs, n_pages, page_size, kv_heads, d_h, ATP_CACHE_E4M3 if e4m3 else ATP_CACHE_SAME)
+
+    def _struct(self) -> _Cache:
+        """What the calls take; the tensors must still lie where they lay."""
+        k, v, ks, vs = self._at
+        if self._K.data_ptr() != k or self._V.data_ptr() != v or (ks is not None and (self._K_scale.data_ptr() != ks or self._V_scale.data_ptr() != vs)):
+            raise ValueError("a tensor of the cache has moved since the cache was made of it")
+        return self._c
 
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, page_size: int, d_h: int, dtype: torch.dtype, device="cuda") -> "PagedCache":
@@ -485,6 +493,10 @@ class PagedCache:
         codes = lambda: torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype)
         scale = lambda: torch.zeros(shape[:3], dtype=torch.uint8, device=device)
         return cls(codes(), codes(), scale(), scale())
+
+
+for _name in PagedCache._NAMES:
+    setattr(PagedCache, _name, property(attrgetter("_" + _name)))
 
 
 def _one_device(first: torch.Tensor, *ts) -> torch.device:
@@ -534,17 +546,17 @@ def _serve(fn, dev: torch.device, *args) -> None:
 
 def _new_rows(cache: PagedCache, K: torch.Tensor, V: torch.Tensor):
     """Type and row strides of packed keys and values that go with a cache."""
-    if V.shape != K.shape or V.dtype is not K.dtype or not (cache.e4m3 or K.dtype is cache.K.dtype):
+    if V.shape != K.shape or V.dtype is not K.dtype or not (cache._e4m3 or K.dtype is cache._K.dtype):
         raise ValueError("K / V shape or dtype mismatch")
-    return _dt(K), _rows(K, "K", cache.kv_heads, cache.d_h), _rows(V, "V")
+    return _dt(K), _rows(K, "K", cache._kv_heads, cache._d_h), _rows(V, "V")
 
 
 def cache_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor) -> None:
     """Rows of the new tokens K, V [tokens, kv_heads, d_h] into their pages: token i of the n new ones of sequence s goes to position
     length[s] - n + i, page table[s, position // page_size].  offsets [n_seq + 1]: where each sequence's tokens start."""
-    dev = _one_device(cache.K, K, V, table, length, offsets)
+    dev = _one_device(cache._K, K, V, table, length, offsets)
     t, ldk, ldv = _new_rows(cache, K, V)
-    _serve(lib.atp_cache_write, dev, cache._c, _batch(table, length, offsets, K.shape[0]), K.data_ptr(), V.data_ptr(), ldk, ldv, t)
+    _serve(lib.atp_cache_write, dev, cache._struct(), _batch(table, length, offsets, K.shape[0]), K.data_ptr(), V.data_ptr(), ldk, ldv, t)
 
 
 def cache_read(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, offsets: torch.Tensor, tokens: Optional[int] = None,
@@ -553,14 +565,14 @@ def cache_read(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, off
     outside every sequence stay.  Without it `tokens` (the rows to make, zeros outside every sequence) is wanted, and for an 8-bit cache
     `dtype`."""
     if out is None:
-        if tokens is None or (dtype is None and cache.e4m3):
+        if tokens is None or (dtype is None and cache._e4m3):
             raise ValueError("without `out`, tokens (and dtype for an 8-bit cache) must be given")
-        dt = cache.K.dtype if dtype is None else dtype
-        out = tuple(torch.zeros((tokens, cache.kv_heads, cache.d_h), dtype=dt, device=cache.device) for _ in range(2))
+        dt = cache._K.dtype if dtype is None else dtype
+        out = tuple(torch.zeros((tokens, cache._kv_heads, cache._d_h), dtype=dt, device=cache._device) for _ in range(2))
     K, V = out
-    dev = _one_device(cache.K, K, V, table, length, offsets)
+    dev = _one_device(cache._K, K, V, table, length, offsets)
     t, ldk, ldv = _new_rows(cache, K, V)
-    _serve(lib.atp_cache_read, dev, cache._c, _batch(table, length, offsets, K.shape[0]), K.data_ptr(), V.data_ptr(), ldk, ldv, t)
+    _serve(lib.atp_cache_read, dev, cache._struct(), _batch(table, length, offsets, K.shape[0]), K.data_ptr(), V.data_ptr(), ldk, ldv, t)
     return K, V
 
 
@@ -617,16 +629,16 @@ def attention_paged(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, len
                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the new tokens Q [tokens, heads, d_h] over the pages of their sequence (their own keys are there already).
     max_new: the largest number of new tokens of a sequence, if known (a hint)."""
-    dev = _one_device(cache.K, Q, table, length, offsets, workspace, out)
-    ldq = _rows(Q, "Q", None, cache.d_h)
+    dev = _one_device(cache._K, Q, table, length, offsets, workspace, out)
+    ldq = _rows(Q, "Q", None, cache._d_h)
     t = _dt(Q)
-    if not cache.e4m3 and Q.dtype != cache.K.dtype:
+    if not cache._e4m3 and Q.dtype != cache._K.dtype:
         raise ValueError("Q and the cache differ in dtype")
     out, ldo = _like_queries(Q, out)
     b = _batch(table, length, offsets, Q.shape[0])
     heads = Q.shape[1]
     keep, ws, ws_bytes = _scratch(lib.atp_attention_paged_workspace(cache._c, b, heads, max_new, t), Q, workspace)
-    _serve(lib.atp_attention_paged, dev, Q.data_ptr(), cache._c, b, out.data_ptr(), ldq, ldo, heads, 1 if causal else 0, scale, max_new,
+    _serve(lib.atp_attention_paged, dev, Q.data_ptr(), cache._struct(), b, out.data_ptr(), ldq, ldo, heads, 1 if causal else 0, scale, max_new,
            ws, ws_bytes, t)
     return out
 
