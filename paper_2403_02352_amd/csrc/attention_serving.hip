@@ -1049,7 +1049,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(ServeArgs a, ServePlan p
     typedef float Share __attribute__((ext_vector_type(NF)));
     const int hk = blockIdx.x % a.kv_heads;
     ServeItem it;
-    if (!serve_item<ROWS_, KT_>(a, p, blockIdx.x / a.kv_heads, false, it) || it.nch < 2) return;
+    if (!serve_item<ROWS_, KT_>(a, p, blockIdx.x / a.kv_heads, false, it)) return;
     const unsigned group = a.heads / a.kv_heads;
     const int l32 = threadIdx.x & 31, row = it.row0 + JOIN * (int)blockIdx.y + (int)(threadIdx.x >> 5);
     if (row >= it.rows) return;   // (whole halves of a wave: the exchanges below stay within one)
@@ -1096,21 +1096,34 @@ __global__ void __launch_bounds__(256) attn_join_kernel(ServeArgs a, ServePlan p
     }
 }
 
-// Items and partial rows that the lengths on the device can lead to, from the sizes that the host knows.  With chunks of at least
-// total / target tiles a cut sequence has fewer than 2·tiles/chunk chunks, so all cut row tiles together have fewer than 2·target.  Keys are not
-// cut where the row tiles of the tokens fill the chip by themselves: no partial rows, no second launch.
-ServePlan plan_of(const ServeArgs& a, int rows, int kt, int wanted, int min_chunk) {
+// Items and partial rows that the lengths on the device can lead to, from the sizes that the host knows.  Chunks hold at least share·total / target
+// key tiles, and a cut sequence has fewer than 2·tiles/chunk of them, so all cut row tiles are fewer than target / share and have fewer than
+// 2·target / share chunks between them.
+// Where the row tiles of the tokens are enough for the chip, packed keys are not cut (no partial rows, no second launch: a long prompt has many row tiles itself),
+// and pages only for sequences that would be at it long after the others: of more than FAR keys, into chunks of at least two target-ths of such sequences' work.
+// A token over 65536 keys beside 8 chunks of 512 of 512, us, uncut / cut: 1250 / 148 (the two by themselves 49 and 63), beside 12 of 4096 1590 / 500 to 600; where
+// nothing is as long, but the table has room for it, the second launch costs 5 to 10 us: 8 chunks of 512 47 / 52, 16 of 512 over 2048 keys 313 / 321.
+constexpr int FAR = 4096;
+
+ServePlan plan_of(const ServeArgs& a, bool paged, int rows, int kt, int wanted, int min_chunk) {
     ServePlan p;
     const int64_t all_rows = (int64_t)a.tokens * (a.heads / a.kv_heads), key_tiles = ((int64_t)a.max_kv + kt - 1) / kt;
     const int64_t tiles = all_rows / rows + std::min<int64_t>(a.n_seq, a.tokens);
     const int64_t target = std::max(1, wanted / a.kv_heads);
-    const bool cut = all_rows / rows < target && a.max_kv > 512;   // (up to 512 keys the second launch costs more than it saves)
-    const int64_t cuts = cut ? std::min<int64_t>((key_tiles + min_chunk - 1) / min_chunk, 2 * target) : 1;
-    p.target = cut ? (int)target : 1;
-    p.min_chunk = cut ? min_chunk : 1 << 30;
-    p.tiles = (int)tiles;
-    p.items = (int)(cut ? std::min(tiles + target, tiles * cuts) : tiles);
-    p.part_rows = cut ? std::min<int64_t>(2 * target * rows, cuts * all_rows) : 0;
+    const bool full = all_rows / rows >= target;
+    const bool cut = full ? paged && a.max_kv > FAR && target > 1 : a.max_kv > 512;   // (up to 512 keys the second launch costs more than it saves)
+    if (!cut) {
+        p.items = (int)tiles;
+        return p;
+    }
+    p.target = (int)target;
+    p.share = full ? 2 : 1;
+    p.above = full ? FAR / kt : 0;
+    p.min_chunk = full ? FAR / kt : min_chunk;
+    const int64_t cuts = std::min<int64_t>((key_tiles + p.min_chunk - 1) / p.min_chunk, 2 * target);
+    p.cut_tiles = (int)std::min(tiles, target / p.share);
+    p.items = (int)std::min(tiles + target, tiles * cuts);
+    p.part_rows = std::min<int64_t>(2 * target / p.share * rows, cuts * all_rows);
     return p;
 }
 
@@ -1130,8 +1143,12 @@ bool few_rows(const ServeArgs& a, int elem_bytes, int64_t max_new) {
 // (wanted items and smallest chunk by measurement, us: 64 sequences of 256 to 8192 keys, e4m3, 512 / 768 / 1024 / 1536 / 2048 items 81 / 80 / 83 / 89 / 90,
 // 6 of 16384 to 65536 keys 199 / 190 / 190 / 179 / 185, 32 of 100 to 20000 82 / 75 / 82 / 84 / 91; one of 32768 keys in chunks of at least 256 / 512 keys
 // 40 / 29; 1238 new tokens over 3000 to 16384 keys, 1024 items of at least 256 / 512 keys 287 / 279; fp32, 150 over 100 to 2000, at least 128 / 256 keys 28 / 43)
-ServePlan plan_bf16(const ServeArgs& a, bool few) { return few ? plan_of(a, ROWS_S, KT_S, 768, 16) : plan_of(a, ROWS, KT, 1024, 8); }
-ServePlan plan_f32(const ServeArgs& a, bool few) { return few ? plan_of(a, 32, 128, 512, 2) : plan_of(a, 128, 32, 512, 4); }
+ServePlan plan_bf16(const ServeArgs& a, KvSource src, bool few) {
+    return few ? plan_of(a, src != KV_PACKED, ROWS_S, KT_S, 768, 16) : plan_of(a, src != KV_PACKED, ROWS, KT, 1024, 8);
+}
+ServePlan plan_f32(const ServeArgs& a, KvSource src, bool few) {
+    return few ? plan_of(a, src != KV_PACKED, 32, 128, 512, 2) : plan_of(a, src != KV_PACKED, 128, 32, 512, 4);
+}
 
 size_t part_bytes(const ServeArgs& a, const ServePlan& p) { return (size_t)p.part_rows * a.kv_heads * (padded_width(a.dh) * 4 + 8); }
 
@@ -1143,7 +1160,7 @@ dim3 grid_of(const ServeArgs& a, ServePlan& p) {
 
 template <int DP>
 hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool few, void* workspace) {
-    ServePlan p = plan_bf16(a, few);
+    ServePlan p = plan_bf16(a, src, few);
     p.part_o = reinterpret_cast<float*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.part_rows * a.kv_heads * DP);
     const float c = a.scale * 1.4426950408889634f;
@@ -1179,7 +1196,7 @@ hipError_t launch_tiles(hipStream_t st, const ServeArgs& a, KvSource src, bool f
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part_rows) return e;
-    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads), (few ? ROWS_S : ROWS) / JOIN);
+    const dim3 join((unsigned)((int64_t)p.cut_tiles * a.kv_heads), (few ? ROWS_S : ROWS) / JOIN);
     if (few) hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS_S, KT_S>), join, dim3(256), 0, st, a, p, c);
     else hipLaunchKernelGGL((attn_join_kernel<bf16_t, DP, ROWS, KT>), join, dim3(256), 0, st, a, p, c);
     return hipGetLastError();
@@ -1195,16 +1212,16 @@ hipError_t launch_f32(hipStream_t st, const ServeArgs& a, KvSource src, ServePla
     else hipLaunchKernelGGL((attn_f32_tiles_kernel<DP, KS, KV_PAGED_E4M3>), grid, dim3(256), 0, st, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.part_rows) return e;
-    const dim3 join((unsigned)((int64_t)p.tiles * a.kv_heads), 128 / KS / JOIN);
+    const dim3 join((unsigned)((int64_t)p.cut_tiles * a.kv_heads), 128 / KS / JOIN);
     hipLaunchKernelGGL((attn_join_kernel<float, DP, 128 / KS, 32 * KS>), join, dim3(256), 0, st, a, p, a.scale * 1.4426950408889634f);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t serve_attention_workspace(const ServeArgs& a, KvSource, int elem_bytes, int64_t max_new) {
+size_t serve_attention_workspace(const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new) {
     const bool few = few_rows(a, elem_bytes, max_new) && (elem_bytes == 2 || a.dh <= 128);
-    return (part_bytes(a, elem_bytes == 2 ? plan_bf16(a, few) : plan_f32(a, few)) + 255) & ~(size_t)255;
+    return (part_bytes(a, elem_bytes == 2 ? plan_bf16(a, src, few) : plan_f32(a, src, few)) + 255) & ~(size_t)255;
 }
 
 hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int elem_bytes, int64_t max_new, void* workspace) {
@@ -1213,7 +1230,7 @@ hipError_t serve_attention(hipStream_t st, const ServeArgs& a, KvSource src, int
     if (elem_bytes == 2)
         return dp == 64 ? launch_tiles<64>(st, a, src, few, workspace) : dp == 128 ? launch_tiles<128>(st, a, src, few, workspace) : launch_tiles<256>(st, a, src, few, workspace);
     few = few && dp <= 128;   // (four shares of 256 features do not fit the LDS)
-    const ServePlan p = plan_f32(a, few);
+    const ServePlan p = plan_f32(a, src, few);
     if (dp == 64) return few ? launch_f32<64, 4>(st, a, src, p, workspace) : launch_f32<64, 1>(st, a, src, p, workspace);
     if (dp == 128) return few ? launch_f32<128, 4>(st, a, src, p, workspace) : launch_f32<128, 1>(st, a, src, p, workspace);
     return launch_f32<256, 1>(st, a, src, p, workspace);

@@ -29,11 +29,12 @@ enum KvSource { KV_PACKED = 0, KV_PAGED = 1, KV_PAGED_E4M3 = 2 };
 hipError_t cache_write_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3);
 hipError_t cache_read_rows(hipStream_t st, const ServeArgs& a, int elem_bytes, bool e4m3);
 
-// How the keys of a call are dealt: about `target` items a key head, of at least `min_chunk` key tiles, partial results of a sequence
-// whose keys are cut go to part_o (rows of floats) and part_ml (maximum and sum of a row).
+// How the keys of a call are dealt: about `target` items a key head, of at least `min_chunk` key tiles; partial results of a sequence
+// whose keys are cut go to part_o (rows of floats) and part_ml (maximum and sum of a row).  part_rows 0: nothing is cut.
 struct ServePlan {
     int target = 1, min_chunk = 1;
-    int tiles = 0, items = 0;   // bounds of the row tiles and of the items of a key head
+    int above = 0, share = 1;   // sequences of more than `above` key tiles are cut, into chunks of at least `share` target-ths of what their row tiles go through
+    int cut_tiles = 0, items = 0;   // bounds of the row tiles whose keys are cut and of the items of a key head
     int per_row = 1;            // items of a key head that a row of the grid holds
     int64_t part_rows = 0;      // bound of the partial rows of a key head
     float* part_o = nullptr;
@@ -58,9 +59,9 @@ struct ServeItem {
 };
 
 // Item w of a key head, the same for every thread of a wave; false behind the last.  Every wave finds it by itself from the lengths on the
-// device: the key tiles that all row tiles go through, over the number of items wanted, give the size of a chunk; then the sequences'
-// items are counted up, a sequence a lane, or a block of sequences a lane and then one a lane.  The host knows none of the lengths, so calls can be captured, and the deal is even for
-// any of them.  With `chunks` off, item w is row tile w.  Row tiles come in descending order: the last ones see the most keys.
+// device: the key tiles that all row tiles go through (of sequences that may be cut), over the number of items wanted, give the size of a chunk; then the sequences'
+// items are counted up, a sequence a lane, or a block of sequences a lane and then one a lane.  The host knows none of the lengths, so calls can be captured.
+// With `chunks` off, item w is row tile w of those whose keys are cut.  Row tiles come in descending order: the last ones see the most keys.
 template <int ROWS, int KT>
 __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& p, int w, bool chunks, ServeItem& it) {
     const int lane = threadIdx.x & 63;
@@ -78,24 +79,30 @@ __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& 
     const int steps = min(a.n_seq, 64);   // (lanes from n_seq on hold nothing: the exchanges stop there)
     const bool cut = p.part_rows > 0;
     const int block = (a.n_seq + 63) / 64;   // sequences of a lane where there are more than lanes
-    int chunk = 1 << 30;
-    if (cut) {
-        // (in floats, a little more than the share: the bound on the cuts holds whatever the sum's rounding)
-        float total = 0.f;
+    int chunk = 1 << 30, uncut = 0;
+    float total = 0.f;
+    if (cut || block > 1) {
 #pragma unroll 4
         for (int i = 0; i < block; ++i) {
             look(lane * block + i);
-            total += (float)row_tiles() * (float)key_tiles();
+            uncut += row_tiles();
+            total += key_tiles() > p.above ? (float)row_tiles() * (float)key_tiles() : 0.f;
         }
+    }
+    bool cuts = false;   // whether there is a sequence to cut
+    if (cut) {
+        // (in floats, a little more than the share: the bound on the cuts holds whatever the sum's rounding)
         for (int off = 1; off < steps; off <<= 1) total += __shfl_xor(total, off);
         const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(total)));
-        chunk = max((int)fminf(all * 1.0001f / (float)p.target + 1.f, 1e9f), p.min_chunk);
+        cuts = all > 0.f;
+        if (cuts) chunk = max((int)fminf(all * (1.0001f * (float)p.share) / (float)p.target + 1.f, 1e9f), p.min_chunk);
     }
+    if (!cuts && !chunks) return false;
     int before = 0, part = 0, s0 = 0;
     // items and partial rows of the sequence looked at last
     const auto count = [&](int& items, int& rows) {
         const int nch = (key_tiles() + chunk - 1) / chunk;
-        items = chunks ? row_tiles() * nch : row_tiles();
+        items = chunks ? row_tiles() * nch : nch > 1 ? row_tiles() : 0;
         rows = nch > 1 ? (int)min((int64_t)((unsigned)n * group) * nch, (int64_t)1 << 22) : 0;
     };
     // sums over the lanes up to this one
@@ -107,15 +114,19 @@ __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& 
         return v;
     };
     if (block > 1) {   // the lane whose sequences hold item w, then those sequences, one a lane
-        int mine = 0, mine_part = 0, items, rows;
+        int mine = uncut, mine_part = 0;
+        if (cuts) {
+            mine = 0;
 #pragma unroll 4
-        for (int i = 0; i < block; ++i) {
-            look(lane * block + i);
-            count(items, rows);
-            mine += items;
-            mine_part = min(mine_part + rows, 1 << 24);
+            for (int i = 0; i < block; ++i) {
+                int items, rows;
+                look(lane * block + i);
+                count(items, rows);
+                mine += items;
+                mine_part = min(mine_part + rows, 1 << 24);
+            }
         }
-        const int upto = scan(mine), upto_part = scan(mine_part);
+        const int upto = scan(mine), upto_part = cuts ? scan(mine_part) : 0;
         const unsigned long long behind = __builtin_amdgcn_ballot_w64(upto > w);
         if (!behind) return false;
         const int at = __builtin_ctzll(behind);
@@ -128,7 +139,7 @@ __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& 
         if (!cut || block > 1) look(s0 + lane < s1 ? s0 + lane : a.n_seq);
         int mine, mine_part;
         count(mine, mine_part);
-        const int upto = scan(mine), upto_part = cut ? scan(mine_part) : 0;
+        const int upto = scan(mine), upto_part = cuts ? scan(mine_part) : 0;
         const unsigned long long behind = __builtin_amdgcn_ballot_w64(lane < steps && before + upto > w);
         if (behind) {
             const int at = __builtin_ctzll(behind);

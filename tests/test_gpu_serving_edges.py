@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_serving import atp, host, ints  # noqa: F401
+from oracle import serving as so
+from test_gpu_serving import TORCH, Pages, atp, check, host, ints, offsets_of, randn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,79 @@ def test_scores_of_256_features_in_fp32_are_short_sums(atp):
         off = (host(got)[::2, 0, 0] - want) / (want * (1 - want))
         print(f"scores off by {mean(off):.3e}, short sums {short:.3e}, long {long:.3e}", flush=True)
         assert mean(off) <= 1.07 * short
+
+
+# ------------------------------------------------------------------ one long sequence among enough rows for the chip
+LONG = [
+    # dtype, cache, lengths, new tokens, heads, kv_heads, d_h, page size, what max_new says
+    ("bf16", "same", [300] * 10 + [9000, 5000], [220] * 10 + [1, 3], 64, 64, 64, 64, 0),                            # row tiles of 128
+    ("bf16", "e4m3", [9001] + [250] * 17, [70] + [250] * 17, 32, 16, 128, 16, 0),
+    ("bf16", "same", [33] * 400 + [8200], [1] * 401, 64, 64, 64, 32, 1),                                            # of 32
+    ("bf16", "e4m3", [20000] + [33] * 400, [2] + [1] * 400, 64, 64, 80, 64, 0),
+    ("f32", "same", [9000] + [300] * 5, [5] + [300] * 5, 48, 48, 64, 64, 0),                                        # fp32, of 128
+    ("f32", "e4m3", [60] * 80 + [12345], [2] * 80 + [1], 256, 256, 64, 32, 2),                                      # fp32, of 32
+    ("f32", "same", [9000] + [700] * 3, [5] + [700] * 3, 32, 32, 136, 128, 0),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", LONG, ids=lambda c: f"{c[0]}-{c[1]}-{c[6]}-{c[8]}")
+def test_a_long_sequence_among_many_rows(atp, case, causal):
+    """More new rows than the call wants items for, and a sequence or two of thousands of keys: those keys are cut.  Three heads and a few sequences are
+    compared with the oracle, every row is finite, a second call gives the same bits."""
+    dtype, kind, lengths, new, heads, hk, d, page, max_new = case
+    print(f"long {case[:2]} {case[4:]} {causal}", flush=True)
+    rng = np.random.default_rng(72)
+    p = Pages(atp, rng, lengths, hk, d, page, dtype, kind, most=-(-max(lengths) // page) + 3, fill=False)
+    n = sum(lengths)
+    K, V = (torch.randn((n, hk, d), generator=torch.Generator("cuda").manual_seed(s), device="cuda").to(TORCH[dtype]) for s in (1, 2))
+    of_keys = offsets_of(lengths)
+    table, length = ints(p.table), ints(lengths)
+    atp.cache_write(p.cache, K, V, table, length, ints(of_keys))
+    if kind == "e4m3":
+        K, V = atp.cache_read(p.cache, table, length, ints(of_keys), tokens=n, dtype=torch.float32)
+    offs = offsets_of(new)
+    Q = randn(rng, (sum(new) + 1, heads, d), dtype, 2.0)
+    out = torch.full_like(Q, 7.0)
+    ws = torch.full((atp.attention_paged_workspace(p.cache, len(lengths), p.table.shape[1], sum(new) + 1, heads, TORCH[dtype], max_new),), 255, dtype=torch.uint8, device="cuda")
+    call = lambda out: atp.attention_paged(Q, p.cache, table, length, ints(offs), causal=causal, max_new=max_new, workspace=ws, out=out)  # noqa: E731
+    got = call(out)
+    torch.cuda.synchronize()
+    assert torch.isfinite(got.float()).all() and (got[sum(new):] == 7.0).all()
+    assert torch.equal(call(torch.full_like(Q, 7.0)), got)
+    some = sorted({*np.argsort(lengths)[-2:].tolist(), 0, len(lengths) // 2, len(lengths) - 1})
+    for s in some:
+        rows, keys = slice(offs[s], min(offs[s + 1], offs[s] + 20)), slice(of_keys[s], of_keys[s + 1])
+        m = rows.stop - rows.start
+        held = lengths[s] - (new[s] - m)   # (the first rows of the sequence: as if the later ones were not there yet)
+        for h in (0, heads // 2 + 1, heads - 1):
+            one = lambda x, at: [host(x[keys, at:at + 1])[:held if causal else None]]  # noqa: E731
+            want = so.attention(host(Q[rows, h:h + 1]), one(K, h * hk // heads), one(V, h * hk // heads), [0, m], [held], causal, 0.0)
+            check(host(got[rows, h:h + 1]), *want, dtype, lengths[s])
+
+
+def test_a_long_sequence_among_many_rows_takes_no_longer_than_by_itself(atp):
+    """8 chunks of 512 tokens and one token over 65536 keys: together no more than three times what the two take one after the other."""
+    heads, hk, d, page = 32, 8, 128, 64
+
+    def call(lengths, new):
+        held = np.array(lengths) // page
+        cache = atp.PagedCache.empty(int(held.sum()), hk, page, d, torch.bfloat16)
+        table = np.full((len(lengths), 65536 // page), -1)
+        for s, h in enumerate(held):
+            table[s, :h] = held[:s].sum() + np.arange(h)
+        Q, args = torch.ones((sum(new), heads, d), dtype=torch.bfloat16, device="cuda"), (ints(table), ints(lengths), ints(offsets_of(new)))
+        out = torch.zeros_like(Q)
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        took = []
+        for _ in range(6):
+            start.record()
+            atp.attention_paged(Q, cache, *args, max_new=max(new), out=out)
+            end.record()
+            torch.cuda.synchronize()
+            took.append(start.elapsed_time(end) * 1e3)
+        return min(took)
+
+    chunks, single, both = call([512] * 8, [512] * 8), call([65536], [1]), call([512] * 8 + [65536], [512] * 8 + [1])
+    print(f"chunks {chunks:.0f} us, single {single:.0f}, together {both:.0f}", flush=True)
+    assert both <= 3 * (chunks + single)
