@@ -397,9 +397,11 @@ atp_status atp_norm_factored(const void* P, const void* C, const float* gain, fl
  * -------------------------------------------------------------------------- */
 
 /* Storage of a cache: the type of the call, or 8-bit floats (1 sign, 4 exponent, 3 mantissa bits; largest value 448) with a power of two
- * for every row of d_h elements: element = value · 2^(scale − 127).  Writing takes the smallest power of two (from 2^−127 on) that brings the
- * finite elements of the row into ±448 and rounds to nearest even; elements that are not finite become NaN.  Both factors being exact, what
- * a code stands for is exact in either storage type. */
+ * for every row of d_h elements: element = value · 2^(scale − 127), scale 0 … 254 (255 stands for nothing: what such a row gives is undefined).  Writing takes
+ * the smallest power of two (from 2^−127 on) that brings the finite elements of the row into ±448 and rounds to nearest even; elements that are not finite
+ * become NaN.  Reading and attention take a code for the nearest value of the storage type: exact up to its largest and down to its smallest step (fp32 all
+ * of them, bf16 multiples of 2^−133; smaller ones are rounded).  At the top: elements from 31/32·2^128 on round to 2^128 when they are written, and that is read as
+ * infinity. */
 typedef enum { ATP_CACHE_SAME = 0, ATP_CACHE_E4M3 = 1 } atp_cache_type;
 
 /* Pages of page_size positions (a power of two up to 65536); page p of a cache holds positions of one sequence, which one is said by the

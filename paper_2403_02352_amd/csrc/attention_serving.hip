@@ -143,7 +143,7 @@ __device__ __forceinline__ void copy16_far(const void* p, unsigned lds) {
 }
 #pragma clang diagnostic pop
 
-// eight 8-bit codes as bf16, times the power of two whose biased exponent is `byte` (exact, but for values below the normal range)
+// eight 8-bit codes as bf16, times the power of two whose biased exponent is `byte` (nearest: exact, but for multiples of less than 2^-133)
 __device__ __forceinline__ uint4 expand8(uint2 c, int byte) {
     const float f = __uint_as_float((uint32_t)byte << 23);
     union { bf16x2 h[4]; uint4 u; } o;

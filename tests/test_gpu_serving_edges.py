@@ -129,3 +129,49 @@ def test_a_long_sequence_among_many_rows_takes_no_longer_than_by_itself(atp):
     chunks, single, both = call([512] * 8, [512] * 8), call([65536], [1]), call([512] * 8 + [65536], [512] * 8 + [1])
     print(f"chunks {chunks:.0f} us, single {single:.0f}, together {both:.0f}", flush=True)
     assert both <= 3 * (chunks + single)
+
+
+# ------------------------------------------------------------------ every code under every exponent
+def _all_codes(atp, page):
+    """A cache of one head of 256 features with the codes 0 to 255 under each of the exponents 0 to 254, a position an exponent; and what they stand for."""
+    cache = atp.PagedCache.empty(256 // page, 1, page, 256, torch.float8_e4m3fn)
+    codes = torch.arange(256, dtype=torch.int32).to(torch.uint8)
+    byte = torch.arange(256).clamp(max=254)   # (the last position repeats the last exponent)
+    for pages, scale in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)):
+        pages.view(torch.uint8).copy_(codes.expand(pages.shape))
+        scale.copy_(byte.view(scale.shape))
+    return cache, codes.view(torch.float8_e4m3fn).double().numpy()[None] * np.exp2(byte.double().numpy() - 127)[:, None]
+
+
+def _rounded(exact, dtype):
+    """Nearest value of the type, ties to even, infinity where that is 2^128 (an intermediate rounding to fp32 is none: codes have four bits)."""
+    return torch.from_numpy(exact).float().to(TORCH[dtype]).double().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_code_under_every_exponent_is_read_as_the_nearest_value(atp, dtype):
+    """Exact from the smallest step of the type on; 2^128 and above are infinite, and what lies below bf16's smallest step is rounded to it or to zero."""
+    cache, exact = _all_codes(atp, 16)
+    K, V = atp.cache_read(cache, ints(np.arange(16)[None]), ints([256]), ints([0, 256]), tokens=256, dtype=TORCH[dtype])
+    want = _rounded(exact, dtype)
+    for got in (K, V):
+        assert np.array_equal(host(got)[:, 0], want, equal_nan=True)
+    step = 2.0 ** (-133 if dtype == "bf16" else -149)
+    inside = (np.abs(exact) < 2.0 ** 128) & (exact % step == 0)
+    assert np.array_equal(want[inside], exact[inside]) and np.isinf(want[np.abs(exact) >= 2.0 ** 128]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 200])
+def test_every_code_under_every_exponent_is_attended_as_its_value(atp, dtype, rows):
+    """One key a sequence: its weight is 1, so O is what reading gives, not finite where that is not.  The key itself is zeros: under the last exponents its score
+    would be infinite or NaN."""
+    cache, exact = _all_codes(atp, 1)
+    cache.K.view(torch.uint8).zero_()
+    Q = torch.zeros((256 * rows, 1, 256), dtype=TORCH[dtype], device="cuda")
+    got = atp.attention_paged(Q, cache, ints(np.arange(256)[:, None]), ints([1] * 256), ints(rows * np.arange(257)), causal=False, max_new=rows)
+    got = host(got).reshape(256, rows, 256)
+    want = _rounded(exact, dtype)
+    fine = np.isfinite(want)
+    for r in (0, rows - 1):
+        assert np.array_equal(got[:, r][fine], want[fine]) and not np.isfinite(got[:, r][~fine]).any()
