@@ -175,3 +175,155 @@ def test_every_code_under_every_exponent_is_attended_as_its_value(atp, dtype, ro
     fine = np.isfinite(want)
     for r in (0, rows - 1):
         assert np.array_equal(got[:, r][fine], want[fine]) and not np.isfinite(got[:, r][~fine]).any()
+
+
+# ------------------------------------------------------------------ values that are not finite where keys are cut
+SPOILT = [
+    # dtype, cache, lengths, new tokens, heads, kv_heads, d_h, page size, spoilt positions of the sequences
+    ("bf16", "same", [3000, 700], [200, 150], 4, 1, 64, 64, [[2850, 2910, 2999], [600]]),       # row tiles of 128
+    ("bf16", "same", [3000, 700], [200, 150], 4, 1, 80, 16, [[2850, 2910, 2999], [600]]),
+    ("bf16", "e4m3", [3000, 700], [200, 150], 2, 1, 128, 64, [[2850, 2910, 2999], [600]]),
+    ("bf16", "e4m3", [2000], [130], 2, 2, 256, 32, [[1900, 1999]]),
+    ("bf16", "same", [4000, 900], [20, 7], 3, 1, 128, 64, [[3985, 3999], [896]]),               # of 32
+    ("bf16", "same", [4000, 900], [20, 7], 3, 1, 72, 16, [[3985, 3999], [896]]),
+    ("bf16", "e4m3", [4000, 900], [20, 7], 3, 1, 64, 32, [[3985, 3999], [896]]),
+    ("f32", "same", [2000, 700], [100, 90], 2, 1, 64, 16, [[1930, 1999], [650]]),               # fp32, of 128
+    ("f32", "e4m3", [2000, 700], [100, 90], 2, 1, 128, 64, [[1930, 1999], [650]]),
+    ("f32", "same", [1500], [20], 2, 1, 200, 64, [[1485, 1499]]),
+    ("f32", "same", [3000, 600], [10, 5], 2, 1, 64, 64, [[2993, 2999], [597]]),                 # of 32
+    ("f32", "e4m3", [3000, 600], [10, 5], 2, 1, 128, 16, [[2993, 2999], [597]]),
+]
+
+
+@pytest.mark.parametrize("case", SPOILT, ids=lambda c: f"{c[0]}-{c[1]}-{c[3][0]}-{c[6]}")
+def test_masked_values_that_are_not_finite_where_keys_are_cut(atp, case):
+    """Sequences long enough to be cut, values spoilt (NaN in 8 bits, else infinite) at positions that some of the new tokens see: those before do not
+    notice, the others not in the other features."""
+    dtype, kind, lengths, new, heads, hk, d, page, spoilt = case
+    print(f"spoilt {case[:2]} {case[2:8]}", flush=True)
+    rng = np.random.default_rng(73)
+    p = Pages(atp, rng, lengths, hk, d, page, dtype, kind)
+    offs, hit = offsets_of(new), np.zeros(sum(new), bool)
+    for s, positions in enumerate(spoilt):
+        for at in positions:
+            no, slot = so.place(p.table[s], at, page, p.n_pages)
+            x = p.cache.V[no].float()
+            x[:, slot, 3] = float("nan") if kind == "e4m3" else float("inf")
+            p.cache.V[no] = x.to(p.cache.V.dtype)
+        hit[offs[s]:offs[s + 1]] = np.arange(lengths[s] - new[s], lengths[s]) >= min(positions)
+    assert hit.any() and not hit.all()
+    assert atp.attention_paged_workspace(p.cache, len(lengths), p.table.shape[1], sum(new), heads, TORCH[dtype]) > 0   # (keys may be cut)
+    Q = randn(rng, (sum(new), heads, d), dtype, 2.0)
+    K, V, present = p.gathered()
+    with np.errstate(invalid="ignore"):
+        want = so.attention(host(Q), K, V, offs, lengths, True, 0.0, present)
+    got = host(atp.attention_paged(Q, p.cache, ints(p.table), ints(lengths), ints(offs), max_new=max(new)))
+    check(got[~hit], *(x[~hit] for x in want), dtype, max(lengths))
+    rest = np.arange(d) != 3
+    check(got[..., rest], want[0][..., rest], want[1][..., rest], want[2], want[3], dtype, max(lengths))
+    assert not np.isfinite(got[hit][..., 3]).any()
+
+
+def test_a_value_that_is_not_finite_costs_its_key_tile(atp):
+    """In a prompt of 6000 tokens what it costs in one of 192, by the keys that are added row by row.  The value stands 64 tokens from the end, in the key tile
+    5888 to 5951 (128 to 191), which the row tile 5888 to 5999 (128 to 191) crosses: of its 112 (64) rows the first 64 see 1 to 64 keys of the tile, 2080 in all,
+    and the other 48 (none) all 64, 3072 in all, so 5152 / 2080 = 2.48 times as many.  Twice that is allowed, for the noise of short times."""
+    rng = np.random.default_rng(74)
+
+    def took(n, spoilt):
+        Q, K, V = (randn(rng, (n, 2, 128), "bf16") for _ in range(3))
+        V[n - 64, :, 7] = float("inf") if spoilt else 1.0
+        offs, out, times = ints([0, n]), torch.zeros_like(Q), []
+        for _ in range(8):
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            atp.attention_packed(Q, K, V, offs, out=out)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(start.elapsed_time(end) * 1e3)
+        return min(times)
+
+    clean, spoilt, short = took(6000, False), took(6000, True), took(192, True)
+    print(f"6000 tokens {clean:.0f} us, spoilt {spoilt:.0f}, 192 spoilt {short:.0f}", flush=True)
+    assert spoilt <= clean + 2 * 2.48 * short
+
+
+# ------------------------------------------------------------------ very many sequences
+def _single_keys(atp, rng, n_seq, long, most_new, dtype, kind, page):
+    """n_seq sequences of one key, those in `long` {sequence: length} longer; pages in order.  -> (cache, lengths, first page of each)"""
+    lengths = np.ones(n_seq, np.int64)
+    for s, n in long.items():
+        lengths[s] = n
+    held = -(-lengths // page)
+    first = np.concatenate([[0], np.cumsum(held)])
+    cache = atp.PagedCache.empty(int(first[-1]), 1, page, 64, torch.float8_e4m3fn if kind == "e4m3" else TORCH[dtype])
+    for x, seed in ((cache.K, 3), (cache.V, 4)):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda"))
+    if kind == "e4m3":
+        cache.K_scale.fill_(127)
+        cache.V_scale.fill_(126)
+    table = first[:-1, None] + np.arange(held.max())
+    table[np.arange(held.max())[None] >= held[:, None]] = -1
+    return cache, lengths, first, ints(table)
+
+
+def _check_single_keys(atp, Q, got, cache, lengths, first, offs, some, dtype):
+    """Sequences of one key give its value, those in `some` what the oracle says."""
+    f = 0.5 if cache.e4m3 else 1.0
+    page = cache.page_size
+    for s in some:
+        rows = slice(offs[s], offs[s + 1])
+        k, v = (host(x[first[s]:first[s + 1], 0].reshape(-1, 1, 64)[:lengths[s]]) for x in (cache.K, cache.V))
+        check(host(got[rows]), *so.attention(host(Q[rows]), [k], [v * f], [0, rows.stop - rows.start], [int(lengths[s])], True, 0.0), dtype, int(lengths[s]))
+    one = torch.ones(len(lengths), dtype=torch.bool)
+    one[list(some)] = False
+    new = np.diff(offs)
+    one &= torch.from_numpy(new == 1)
+    at = one.nonzero()[:, 0]
+    value = cache.V.float().view(-1, page, 64)[torch.from_numpy(first[:-1])[at].cuda(), 0] * f
+    assert torch.equal(got[torch.from_numpy(offs[:-1])[at].cuda()].float(), value[:, None].expand(-1, Q.shape[1], -1).to(TORCH[dtype]).float())
+
+
+@pytest.mark.parametrize("dtype,kind", [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same")])
+def test_thousands_of_sequences_with_long_ones_at_the_end(atp, dtype, kind):
+    """5000 single tokens, a few of them over thousands of keys and late: more than one step of the count within a lane's block, and keys are cut."""
+    rng = np.random.default_rng(75)
+    long = {4300: 1000, 4864: 3000, 4930: 700, 4999: 2500}
+    cache, lengths, first, table = _single_keys(atp, rng, 5000, long, 1, dtype, kind, 32)
+    new = np.ones(5000, np.int64)
+    new[4864] = 9
+    offs = offsets_of(new)
+    assert atp.attention_paged_workspace(cache, 5000, table.shape[1], int(offs[-1]), 2, TORCH[dtype], 9) > 0
+    Q = randn(rng, (int(offs[-1]), 2, 64), dtype, 2.0)
+    for max_new in (0, 9):
+        got = atp.attention_paged(Q, cache, table, ints(lengths), ints(offs), max_new=max_new)
+        _check_single_keys(atp, Q, got, cache, lengths, first, offs, long, dtype)
+
+
+@pytest.mark.parametrize("tokens", ["all", "few"])
+def test_as_many_sequences_as_a_call_takes(atp, tokens):
+    """65536 sequences, three of them long: a new token each (more rows than the chip wants), or new tokens for those three and two others only."""
+    rng = np.random.default_rng(76)
+    n_seq, long = 65536, {0: 9000, 40000: 5000, 65535: 8500}
+    cache, lengths, first, table = _single_keys(atp, rng, n_seq, long, 1, "bf16", "same", 64)
+    new = np.ones(n_seq, np.int64)
+    if tokens == "few":
+        new[:] = 0
+        new[[0, 1023, 1024, 40000, 65535]] = 5, 1, 1, 1, 3
+    offs = offsets_of(new)
+    Q = randn(rng, (int(offs[-1]), 1, 64), "bf16", 2.0)
+    print(f"65536 sequences, {tokens}", flush=True)
+    args = (table, ints(lengths), ints(offs))
+    got = atp.attention_paged(Q, cache, *args, max_new=5)
+    torch.cuda.synchronize()
+    _check_single_keys(atp, Q, got, cache, lengths, first, offs, long, "bf16")
+    K, V = atp.cache_read(cache, *args, tokens=int(offs[-1]))
+    s = torch.from_numpy(np.repeat(np.arange(n_seq), new))
+    at = torch.from_numpy(lengths[s.numpy()] - new[s.numpy()] + np.arange(int(offs[-1])) - offs[s.numpy()])
+    where = torch.from_numpy(first[s.numpy()]) + at // 64
+    assert torch.equal(K[:, 0], cache.K[where.cuda(), 0, (at % 64).cuda()]) and torch.equal(V[:, 0], cache.V[where.cuda(), 0, (at % 64).cuda()])
+    atp.cache_write(cache, K.flip(0), V.flip(0), *args)
+    assert torch.equal(cache.K[where.cuda(), 0, (at % 64).cuda()], K[:, 0].flip(0)) and torch.equal(cache.V[where.cuda(), 0, (at % 64).cuda()], V[:, 0].flip(0))
+    # packed: a token each
+    x = [randn(rng, (n_seq, 1, 64), "bf16") for _ in range(3)]
+    assert tokens == "few" or torch.equal(atp.attention_packed(*x, ints(np.arange(n_seq + 1))), x[2])
