@@ -1111,7 +1111,8 @@ ServePlan plan_of(const ServeArgs& a, bool paged, int rows, int kt, int wanted, 
     const int64_t tiles = all_rows / rows + std::min<int64_t>(a.n_seq, a.tokens);
     const int64_t target = std::max(1, wanted / a.kv_heads);
     const bool full = all_rows / rows >= target;
-    const bool cut = full ? paged && a.max_kv > FAR && target > 1 : a.max_kv > 512;   // (up to 512 keys the second launch costs more than it saves)
+    // (a target of one is never cut, a chunk of all there is; up to 512 keys the second launch costs more than it saves)
+    const bool cut = target > 1 && (full ? paged && a.max_kv > FAR : a.max_kv > 512);
     if (!cut) {
         p.items = (int)tiles;
         return p;
