@@ -390,7 +390,8 @@ atp_status atp_norm_factored(const void* P, const void* C, const float* gain, fl
  * each sequence starts: tokens offsets[s] … offsets[s+1] − 1 belong to sequence s (none when both are equal).  Rows outside every sequence
  * are not written, and what they hold reaches nobody.  A token's row of heads·d_h elements is contiguous, rows are a stride (ldq, ldk, ldv, ldo, in elements)
  * apart, so Q, K and V may be column blocks of one packed projection.  Every stride is a multiple of 16 bytes, at least the row and at most 2^24 elements.
- * At most 65536 sequences a call.  `heads` is a multiple of `kv_heads`: query head h reads key head h / (heads / kv_heads).  d_h is a multiple of 8 up to 256.
+ * At most 65536 sequences a call (attention counts them up in every workgroup: beyond a few thousand its time grows with the square of their number, 4096 single
+ * tokens 0.3 ms, 65536 65 ms).  `heads` is a multiple of `kv_heads`: query head h reads key head h / (heads / kv_heads).  d_h is a multiple of 8 up to 256.
  * Offsets are read on the device only: they may change between replays of a captured graph, as long as `tokens` and `n_seq` stay.
  * Values outside 0 … tokens are taken to the nearest bound, a sequence that ends before it starts is empty, and the sequences of offsets
  * that decrease are computed in an undefined way, within the tensors.
@@ -442,8 +443,9 @@ atp_status atp_cache_read(const atp_cache* cache, const atp_batch* batch, void* 
 /* Attention of every sequence over its own tokens:
  *     O[i, h] = Σ_j softmax_j(scale · <Q[i, h], K[j, h / (heads/kv_heads)]>) · V[j, h / (heads/kv_heads)],
  * j over the tokens of the sequence, with `causal` (not 0) those up to i.  scale <= 0: 1/sqrt(d_h).  Values of keys that a query does not
- * see never reach it, also when they are not finite.  A query all of whose scores are −inf gives zeros.
- * Workspace: 0 bytes for some shapes; depends on sizes only.  Scratch of one call: calls that share it must not overlap in time.
+ * see never reach it, also when they are not finite.  A query all of whose scores are −inf gives zeros.  Scores, weights and sums are fp32; in bf16 the weights
+ * are rounded to bf16 for their product with V, as in atp_attention, and their sum is not.
+ * Workspace: 0 bytes for some shapes, at most 137 MB up to d_h 128 and 271 MB above; depends on sizes only.  Scratch of one call: calls that share it must not overlap in time.
  * Errors: ATP_ERR_INVALID_ARG, ATP_ERR_UNSUPPORTED (d_h above 256 or no multiple of 8; more than 65535 key heads; tokens·heads >= 2^31),
  * ATP_ERR_WORKSPACE, ATP_ERR_DEVICE. */
 size_t atp_attention_packed_workspace(int64_t n_seq, int64_t tokens, int heads, int kv_heads, int d_h, atp_dtype t);
@@ -485,7 +487,9 @@ typedef enum {
 void atp_profile_enable(unsigned class_mask); /* bit c enables class c; 0 disables */
 void atp_profile_reset(void);
 /* Sums over the launches recorded since the last reset.  flops / bytes are the
- * ALGORITHMIC counts of those launches.  Returns ATP_ERR_INVALID_ARG for a bad class. */
+ * ALGORITHMIC counts of those launches; the lengths of serving calls are on the
+ * device: atp_attention_packed counts as if its sequences were equally long,
+ * atp_attention_paged no flops and the bytes of Q and O only.  Returns ATP_ERR_INVALID_ARG for a bad class. */
 atp_status atp_profile_read(int kernel_class, double* total_ms, int64_t* launches, double* flops,
                             double* bytes);
 

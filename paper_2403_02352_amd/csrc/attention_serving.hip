@@ -82,7 +82,7 @@ __device__ __forceinline__ void store_row(T* Op, const RowSum& r, int dh) {
 // Where a value that is not finite stands at a key that some rows of a tile do not see, the product of the tile would carry it into every row (zero
 // times infinity is NaN).  Such key tiles, bits of `bad` from tile kt0 on, are left out of the products; here they are added row by row to the
 // sums of 32 rows from row0 on, that lie in LDS (so: DP floats a row, sml: maximum and sum), and the rows are stored.  Only tiles that
-// hold the last keys of a row can be among them, so this is short however long the sequence is.
+// hold the last keys of a row can be among them, so this does not grow with the sequence: 0.6 us a key of a wave's row, 0.7 ms for a tile of 64 keys and 112 rows.
 template <typename T, int SRC, int DP, int KT_>
 __device__ __forceinline__ void finish_by_rows(const ServeArgs& a, const ServePlan& p, const ServeItem& it, int hk, int row0, const float* so, const float2* sml, unsigned bad,
                                                int kt0) {
@@ -373,7 +373,8 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_tiles_kernel(Serv
                 psum += pv;
             }
         l_run += psum;
-        // weights rounded to bf16 for the matrix product; their sum is that of the fp32 values
+        // Weights rounded to bf16 for the matrix product (fp32 operands would run at a sixteenth of its rate); their sum is that of the fp32 values.  The errors of
+        // the keys' weights average out: the output is off by 1.7 to 1.9e-3 (norm, against 64 bits) where its own rounding makes 1.65e-3.
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -707,7 +708,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
         }
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            uint4 pu;   // weights rounded to bf16 for the matrix product
+            uint4 pu;   // weights rounded to bf16 for the matrix product, as in the tiles of 128 rows
             pu.x = pack_bf2(s[8 * tt + 0], s[8 * tt + 1]);
             pu.y = pack_bf2(s[8 * tt + 2], s[8 * tt + 3]);
             pu.z = pack_bf2(s[8 * tt + 4], s[8 * tt + 5]);
@@ -784,9 +785,10 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) attn_few_rows_kernel(S
 // fp32: tiles of 32 rows a wave and 32 keys on v_mfma_f32_32x32x2f32 (products and sums in fp32), scores transposed, a row to a lane.  Accumulator
 // register v of lane half lh belongs to key 8·(v/4) + 4·lh + v%4, so it is at once the operand of a step of Oᵀ += Vᵀ·Pᵀ over the two keys of
 // its halves, and values are read as they lie.  KS = 1: four waves of 32 rows share the keys; KS = 4: one block of 32 rows, its key tiles dealt to
-// four waves that meet at the end (few rows).  Bound by the fp32 matrix cores (256 flop per clock and compute unit) where there is work for all of
-// them: 4 chunks of 128 tokens over 4000 keys, 12 heads of 64, 132 us (47 TFLOP/s); by the chain of loads and products of a stage below that (5 prompts
-// of up to 96 tokens: 11 us).
+// four waves that meet at the end (few rows).  Where there is work for the whole chip a stage's masks and exponentials stand between its products, not beside them, and
+// two barriers around each stage keep the waves in step: two prompts of 4096 tokens, 12 heads of 64, take 710 to 730 us (70 TFLOP/s of the products that count; a large
+// library product reaches 154), matrix cores busy in 55 % of the cycles, vector unit in 39; 4 chunks of 128 tokens over 4000 keys 130 to 140 us (45 TFLOP/s), 50 and
+// 39 %, and the last round of workgroups is not full.  Below that the chain of loads and products of a stage counts (5 prompts of up to 96 tokens: 11 us).
 // ---------------------------------------------------------------------------
 template <int DP, int KS, int SRC>
 __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, ServePlan p) {
@@ -927,7 +929,7 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
         if (key0 > lim_wave1 || bad) continue;
         f32x16 s;
         // The matrix instruction adds one product after the other: sums of 16 features, added up, carry less of a rounding error than one chain.
-        // 256 features take sums of 8, added up over 64: 0.80 of the error of sums of 16 in one row, for a seventh of the time (4 prompts of 2048, 8 heads over 2
+        // 256 features take sums of 8, added up over 64: 0.80 of the error of sums of 16 in one row, for a seventh more time (4 prompts of 2048, 8 heads over 2
         // of 256: 1519 / 1754 us).
         constexpr int NU = DP == 256 ? 1 : 2, NM = DP == 256 ? 8 : DP / 8;   // k-groups of 8 in a sum, in an intermediate one
 #pragma unroll
@@ -1041,6 +1043,8 @@ __global__ void __launch_bounds__(256, 1) attn_f32_tiles_kernel(ServeArgs a, Ser
 
 // Rows whose keys were cut: chunk sums at their common maximum, added in order.  A workgroup takes 8 rows of a row tile of a key head, 32 lanes to
 // a row, which weigh 32 chunks at a time between them and then add up a share of the features each, eight chunks' loads in flight.
+// A chunk weighs 2^y, y = (its maximum - the row's)·scale·log2 e, for fp32 too: four roundings of y (log2 e, its product with the scale, the difference, the product)
+// put the weight off by up to |y|·ln2·4·2^-24 of itself, which is 1.5·2^-24 of the largest weight at most.
 constexpr int JOIN = 8;
 
 template <typename T, int DP, int ROWS_, int KT_>
@@ -1136,7 +1140,7 @@ int padded_width(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 bool few_rows(const ServeArgs& a, int elem_bytes, int64_t max_new) {
     const int64_t group = a.heads / a.kv_heads, most = elem_bytes == 2 ? 64 : 32, rows = a.tokens * group;
     if ((max_new > 0 && max_new <= most / group) || rows <= most * a.n_seq) return true;
-    // fp32 over a few keys, as long as tiles of 32 rows are one round of workgroups: their four waves go through the keys at once instead of one after
+    // fp32 over a few keys (packed: a few tokens in all, for what the host knows), as long as tiles of 32 rows are one round of workgroups: their four waves go through the keys at once instead of one after
     // the other (12 heads of 64, us, tiles of 128 / of 32: 5 prompts of 96 tokens 18.3 / 11.5, of 48 14.0 / 11.4; 16 of 128, two rounds, 22.8 / 31.7)
     return elem_bytes == 4 && a.max_kv <= 512 && (rows / 32 + a.n_seq) * a.kv_heads <= 256;
 }

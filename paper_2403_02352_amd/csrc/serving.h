@@ -61,6 +61,8 @@ struct ServeItem {
 // Item w of a key head, the same for every thread of a wave; false behind the last.  Every wave finds it by itself from the lengths on the
 // device: the key tiles that all row tiles go through (of sequences that may be cut), over the number of items wanted, give the size of a chunk; then the sequences'
 // items are counted up, a sequence a lane, or a block of sequences a lane and then one a lane.  The host knows none of the lengths, so calls can be captured.
+// The count is n_seq / 64 sequences a lane in every workgroup, so with one token a sequence the time grows with the square of their number: 4 heads over 1 of 64,
+// 16 keys each, 1024 sequences 30 us, 4096 300 us, 16384 4.2 ms, 65536 65 ms (in tables of 4096 positions, where keys may be cut, 130 us and 1.0 ms for the first two).
 // With `chunks` off, item w is row tile w of those whose keys are cut.  Row tiles come in descending order: the last ones see the most keys.
 template <int ROWS, int KT>
 __device__ __forceinline__ bool serve_item(const ServeArgs& a, const ServePlan& p, int w, bool chunks, ServeItem& it) {
