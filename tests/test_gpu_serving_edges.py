@@ -227,7 +227,7 @@ def test_masked_values_that_are_not_finite_where_keys_are_cut(atp, case):
 def test_a_value_that_is_not_finite_costs_its_key_tile(atp):
     """In a prompt of 6000 tokens what it costs in one of 192, by the keys that are added row by row.  The value stands 64 tokens from the end, in the key tile
     5888 to 5951 (128 to 191), which the row tile 5888 to 5999 (128 to 191) crosses: of its 112 (64) rows the first 64 see 1 to 64 keys of the tile, 2080 in all,
-    and the other 48 (none) all 64, 3072 in all, so 5152 / 2080 = 2.48 times as many.  Twice that is allowed, for the noise of short times."""
+    and the other 48 (none) all 64, so 5152 / 2080 = 2.48 times as many.  Twice that is allowed, for the noise of short times."""
     rng = np.random.default_rng(74)
 
     def took(n, spoilt):
